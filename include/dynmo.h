@@ -27,7 +27,7 @@
  *     fp32 accumulation, results rounded to nearest-even once.
  *     Logits, scores, gate weights and their gradients are always float.
  *   - weights: Wg, Wu are [E, F, H]; Wd is [E, H, F].
- *   - limits: 1 <= k <= E <= 64 (k <= 8 for the combine calls); for DYNMO_BF16
+ *   - limits: 1 <= k <= E <= 64 (256 for dynmo_route_scored and its backward; k <= 8 for the combine calls); for DYNMO_BF16
  *     H and F must be multiples of 8, for DYNMO_F32 H a multiple of 4.  Violations return DYNMO_EINVAL /
  *     DYNMO_EUNSUPPORTED before anything is launched.
  *     bf16 results are right for H and F up to 2^22 (a tile's rows are addressed with 32-bit byte
@@ -35,7 +35,7 @@
  *     The fp32 path is limited to floor(T*k / 64) + min(E, T*k) <= 65535 (DYNMO_EUNSUPPORTED
  *     beyond).
  *   - NaN in logits or scores is undefined input, and so is a token whose logits are all
- *     -inf (its gate weights would be 0/0).
+ *     -inf (its gate weights would be 0/0); dynmo_route_scored says what it does with them.
  */
 #ifndef DYNMO_H
 #define DYNMO_H
@@ -120,6 +120,40 @@ int32_t dynmo_route_topk_ex(const dynmo_desc* d, const float* logits, const floa
                             int32_t* expert_idx, float* gate_w, void* stream);
 int32_t dynmo_route_topk_all_bwd(const dynmo_desc* d, const float* dgate, const float* logits,
                                  const int32_t* expert_idx, float* dlogits, void* stream);
+
+/* Routing by scores, with what keeps experts balanced without an auxiliary loss (Sec. 2.1: bias terms
+ * added to the token-to-expert affinity scores) and with expert groups, so that a token's experts lie on few workers.  Per token:
+ *   s = softmax over all E logits, or the logistic function of each;  v = s + bias (bias [E] or NULL)
+ *   groups > 1: the experts are `groups` equal runs of indices; a group counts the sum of its group_best (1 or 2) largest v, and
+ *     only the experts of the top_groups groups that count most can be chosen
+ *   slot s gets the expert with the s-th largest v of those that can be chosen
+ *   gate_w = s of the chosen expert, divided by the sum over the chosen ones if renormalize is 1 (zero where that sum is),
+ *     times scale
+ * Equal values: lower index first, groups as experts.  v is compared in 64 bits, from scores computed in 64 bits.  The bias
+ * steers the selection only.
+ * An expert whose logit is NaN or -inf, or whose v is, is never chosen, and its score is zero; a logit of +inf counts as the
+ * largest finite number.  A slot for which no expert is left gets expert_idx -1 and gate_w 0 (a group with fewer than
+ * group_best experts that can be chosen counts those it has).
+ * Needs E a multiple of groups, 1 <= top_groups <= groups and k <= top_groups * (E / groups); E up to 256 here, for a caller
+ * who routes over the experts of several workers and maps the indices to its own (and to -1) before dynmo_permute.
+ * logits [T,E] -> expert_idx [T,k], gate_w [T,k].
+ *
+ * dynmo_route_scored_bwd: the gradient through gate_w; the selection and the bias carry none.  Every element of
+ * dlogits [T,E] is written.  expert_idx entries outside 0 .. E-1 are slots without a gradient, and an expert that stands in two slots gets
+ * the sum.  dgate [T,k], logits [T,E], expert_idx [T,k] -> dlogits [T,E]. */
+enum { DYNMO_SCORE_SOFTMAX = 0, DYNMO_SCORE_SIGMOID = 1 };
+typedef struct dynmo_route_rule {
+  int32_t score;      /* DYNMO_SCORE_* */
+  int32_t groups;     /* 1: no groups */
+  int32_t top_groups;
+  int32_t group_best; /* 1 or 2 */
+  int32_t renormalize; /* 0 or 1 */
+  float scale;        /* finite */
+} dynmo_route_rule;
+int32_t dynmo_route_scored(const dynmo_desc* d, const dynmo_route_rule* rule, const float* logits, const float* bias,
+                           int32_t* expert_idx, float* gate_w, void* stream);
+int32_t dynmo_route_scored_bwd(const dynmo_desc* d, const dynmo_route_rule* rule, const float* dgate, const float* logits,
+                               const int32_t* expert_idx, float* dlogits, void* stream);
 
 /* Expert capacity with token dropping: slots are served in ascending flat order
  * t*k + s and a slot whose expert already holds `capacity` slots is dropped:

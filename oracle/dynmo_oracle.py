@@ -139,6 +139,78 @@ def route_topk_biased_bwd(dgate, logits, expert_idx, norm="selected"):
     return out
 
 
+def route_scores(logits, score):
+    """Scores of the scored router in float64: softmax over all E logits ("softmax") or the logistic function of each
+    ("sigmoid").  NaN and -inf have the score zero; +inf counts as the largest float32."""
+    z = np.asarray(logits, dtype=np.float32)
+    dead = np.isnan(z) | (z == -np.inf)
+    z = np.where(dead, np.float32(0), np.minimum(z, np.finfo(np.float32).max)).astype(F64)
+    out = np.zeros(z.shape, F64)
+    for t in range(z.shape[0]):
+        live = ~dead[t]
+        if not live.any():
+            continue
+        with np.errstate(over="ignore", under="ignore"):
+            if score == "softmax":
+                p = np.exp(z[t, live] - z[t, live].max())
+                out[t, live] = p / p.sum()
+            else:
+                out[t, live] = 1.0 / (1.0 + np.exp(-z[t, live]))
+    return out, dead
+
+
+def route_scored(logits, bias, k, score="softmax", groups=1, top_groups=1, group_best=1, renormalize=True, scale=1.0):
+    """Token-choice routing by scores with a selection bias and expert groups (the balancing without an auxiliary loss
+    that Sec. 2.1 names, and the restriction of a token to few workers' experts).  Order value v = score + bias in float64;
+    a group counts the sum of its group_best largest v (those it has); of the top_groups groups' experts the k with the
+    largest v, ties to the lower index; weights are the chosen scores, divided by their sum if renormalize, times scale.
+    Experts whose logit is NaN or -inf, or whose v is, are never chosen; a slot without an expert is -1 with weight 0.
+    Returns expert_idx int32 [T, k], gate_w f64 [T, k]."""
+    s, dead = route_scores(logits, score)
+    T, E = s.shape
+    size = E // groups
+    with np.errstate(invalid="ignore"):
+        v = s if bias is None else s + _f64(bias)[None, :]
+    idx = np.full((T, k), -1, I32)
+    gate = np.zeros((T, k), F64)
+    for t in range(T):
+        can = [e for e in range(E) if not dead[t, e] and v[t, e] > -np.inf]
+        worth = []
+        for g in range(groups):
+            mine = sorted((v[t, e] for e in can if e // size == g), reverse=True)[:group_best]
+            worth.append(sum(mine) if mine else -np.inf)
+        stay = sorted(range(groups), key=lambda g: (-worth[g], g))[:top_groups]
+        order = sorted((e for e in can if e // size in stay), key=lambda e: (-v[t, e], e))[:k]
+        idx[t, :len(order)] = order
+        w = s[t, order]
+        if renormalize:
+            w = w / w.sum() if w.sum() > 0 else np.zeros_like(w)
+        gate[t, :len(order)] = w * F64(np.float32(scale))
+    return idx, gate
+
+
+def route_scored_bwd(dgate, logits, expert_idx, score="softmax", renormalize=True, scale=1.0):
+    """Gradient of route_scored's weights with respect to the logits (selection and bias carry none), one Jacobian a token."""
+    s, _ = route_scores(logits, score)
+    T, E = s.shape
+    ei = np.asarray(expert_idx)
+    out = np.zeros((T, E), F64)
+    for t in range(T):
+        slots = [j for j in range(ei.shape[1]) if 0 <= ei[t, j] < E]
+        p = s[t, ei[t, slots]]
+        g = _f64(dgate)[t, slots] * F64(np.float32(scale))
+        if renormalize:
+            total = p.sum()
+            if total > 0:  # d(p_i / S) / dp_j = delta_ij / S - p_i / S^2, contracted over i
+                g = (np.eye(len(slots)) / total - np.outer(p, np.ones(len(slots))) / total ** 2).T @ g
+            else:
+                g = np.zeros_like(g)
+        ds = np.zeros(E, F64)
+        np.add.at(ds, ei[t, slots], g)
+        out[t] = ds * s[t] * (1.0 - s[t]) if score == "sigmoid" else s[t] * (ds - (ds * s[t]).sum())
+    return out
+
+
 def capacity_drop(expert_idx, E, capacity):
     """Expert capacity with token dropping (Sec. 6: an expert processes at most
     `capacity` tokens).  Slots are served in ascending flat order i = t*k + s:

@@ -36,9 +36,15 @@ class Desc(C.Structure):
                 ("dtype", C.c_int32)]
 
 
+class Rule(C.Structure):
+    _fields_ = [("score", C.c_int32), ("groups", C.c_int32), ("top_groups", C.c_int32), ("group_best", C.c_int32),
+                ("renormalize", C.c_int32), ("scale", C.c_float)]
+
+
 _P = C.c_void_p
 _I = C.c_int32
 _D = C.POINTER(Desc)
+_R = C.POINTER(Rule)
 
 # name -> (restype, argtypes); mirrors include/dynmo.h one to one
 SIGNATURES = {
@@ -51,6 +57,8 @@ SIGNATURES = {
     "dynmo_route_capacity_bwd": (_I, [_D, _P, _P, _P, _P, _P]),
     "dynmo_route_topk_ex": (_I, [_D, _P, _P, _I, _P, _P, _P]),
     "dynmo_route_topk_all_bwd": (_I, [_D, _P, _P, _P, _P, _P]),
+    "dynmo_route_scored": (_I, [_D, _R, _P, _P, _P, _P, _P]),
+    "dynmo_route_scored_bwd": (_I, [_D, _R, _P, _P, _P, _P, _P]),
     "dynmo_route_drop_workspace_bytes": (C.c_size_t, [_D]),
     "dynmo_route_drop": (_I, [_D, _P, _I, _P, _P, C.c_size_t, _P]),
     "dynmo_permute_workspace_bytes": (C.c_size_t, [_D]),
@@ -149,7 +157,7 @@ def _by_ctypes(name, kinds):
     def call(*args):
         words = []
         for kind, a in zip(kinds, args):
-            if kind == "d":
+            if kind in "dr":
                 words.append(C.byref(a))
             elif kind == "t":
                 words.append(_ptr(a))
@@ -187,6 +195,7 @@ def _calls():
             raise RuntimeError("_fastcall.so is not built: run `python -m paper_2505_14864_amd.build` (or __graft_entry__.build())")
         from . import _fastcall as module
         module.setup(_fail, Desc, torch.cuda.current_device, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+        module.rule(Rule)
         os.register_at_fork(after_in_child=module.forked)
         _fastcall = module
     return _fastcall
@@ -199,7 +208,7 @@ class _launch:
 for _name, _kinds in {
     "dynmo_route_topk": "dttts", "dynmo_route_capacity": "dtiiitts", "dynmo_route_active": "dtitts",
     "dynmo_route_topk_bwd": "dtttts", "dynmo_route_capacity_bwd": "dtttts", "dynmo_route_topk_ex": "dttitts",
-    "dynmo_route_topk_all_bwd": "dtttts", "dynmo_route_drop": "dtitws", "dynmo_permute": "dttttttws",
+    "dynmo_route_topk_all_bwd": "dtttts", "dynmo_route_scored": "drtttts", "dynmo_route_scored_bwd": "drtttts", "dynmo_route_drop": "dtitws", "dynmo_permute": "dttttttws",
     "dynmo_permute_static": "dtttttts", "dynmo_permute_bwd": "dtttts", "dynmo_grouped_ffn_fwd": "dttttttttws",
     "dynmo_grouped_ffn_fwd_gather": "dtttttttttws", "dynmo_grouped_ffn_fwd_combine": "dtttttttttttttws",
     "dynmo_grouped_ffn_bwd": "dttttttttttttws", "dynmo_grouped_ffn_bwd_scatter": "dtttttttttttttttws",
@@ -241,6 +250,22 @@ def dynmo_route_topk_ex(d, logits, bias, gate_norm, expert_idx, gate_w, stream=N
 
 def dynmo_route_topk_all_bwd(d, dgate, logits, expert_idx, dlogits, stream=None):
     _launch.dynmo_route_topk_all_bwd(d, dgate, logits, expert_idx, dlogits, stream)
+
+
+SCORES = ("softmax", "sigmoid")
+
+
+def make_rule(score="softmax", groups=1, top_groups=1, group_best=1, renormalize=True, scale=1.0):
+    """The routing rule of dynmo_route_scored and its backward pass."""
+    return Rule(SCORES.index(score), int(groups), int(top_groups), int(group_best), int(bool(renormalize)), float(scale))
+
+
+def dynmo_route_scored(d, rule, logits, bias, expert_idx, gate_w, stream=None):
+    _launch.dynmo_route_scored(d, rule, logits, bias, expert_idx, gate_w, stream)
+
+
+def dynmo_route_scored_bwd(d, rule, dgate, logits, expert_idx, dlogits, stream=None):
+    _launch.dynmo_route_scored_bwd(d, rule, dgate, logits, expert_idx, dlogits, stream)
 
 
 def dynmo_route_drop_workspace_bytes(d):

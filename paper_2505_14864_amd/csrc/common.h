@@ -30,12 +30,12 @@ inline int32_t hip_fail(hipError_t e) {
 constexpr int kMaxExperts = 64;
 constexpr int kMaxCombineSlots = 8;
 
-inline int32_t check_desc(const dynmo_desc* d) {
+inline int32_t check_desc(const dynmo_desc* d, int max_experts = kMaxExperts) {
   if (!d) return DYNMO_EINVAL;
   if (d->T < 0 || d->H <= 0 || d->F <= 0 || d->E <= 0 || d->k <= 0) return DYNMO_EINVAL;
   if (d->k > d->E) return DYNMO_EINVAL;
   if (d->dtype != DYNMO_F32 && d->dtype != DYNMO_BF16) return DYNMO_EINVAL;
-  if (d->E > kMaxExperts) return DYNMO_EUNSUPPORTED;
+  if (d->E > max_experts) return DYNMO_EUNSUPPORTED;
   if ((int64_t)d->T * d->k >= (int64_t)1 << 30) return DYNMO_EUNSUPPORTED;
   if (d->dtype == DYNMO_BF16 && ((d->H % 8) || (d->F % 8))) return DYNMO_EUNSUPPORTED;
   if (d->dtype == DYNMO_F32 && (d->H % 4)) return DYNMO_EUNSUPPORTED;  // rows move in 16-byte pieces

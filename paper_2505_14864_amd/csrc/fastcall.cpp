@@ -17,10 +17,10 @@ namespace {
 
 constexpr int kMaxWords = 20;
 
-// What the Python side hands over: raises the error of a status; the descriptor's type; torch's current device, by the call that
+// What the Python side hands over: raises the error of a status; the descriptor's type, and the routing rule's; torch's current device, by the call that
 // initialises torch's GPU state (and refuses to in a forked child) and by the quick one that follows; the raw handle of a device's
 // current stream
-PyObject *g_fail = nullptr, *g_desc = nullptr, *g_first_device = nullptr, *g_device = nullptr, *g_stream = nullptr;
+PyObject *g_fail = nullptr, *g_desc = nullptr, *g_rule = nullptr, *g_first_device = nullptr, *g_device = nullptr, *g_stream = nullptr;
 bool g_initialised = false;  // in this process
 
 struct Function {
@@ -30,7 +30,7 @@ struct Function {
   PyObject* name;
   PyObject* by_ctypes;  // the same call with the same arguments
   Py_ssize_t n_args;
-  // one letter per argument: d descriptor, t contiguous GPU tensor or None, w workspace tensor (its pointer and number of
+  // one letter per argument: d descriptor, r routing rule, t contiguous GPU tensor or None, w workspace tensor (its pointer and number of
   // elements), i int, s stream or None
   char kinds[kMaxWords];
 };
@@ -59,9 +59,9 @@ constexpr auto kJumps = jumps(std::make_index_sequence<kMaxWords + 1>());
 
 enum Taken { kPlain, kOther, kError };  // kError: with an exception set
 
-Taken descriptor_of(PyObject* o, uint64_t* p) {
-  if ((PyObject*)Py_TYPE(o) != g_desc) return kOther;
-  Py_buffer b;  // the caller holds the descriptor, and its memory does not move
+Taken structure_of(PyObject* o, PyObject* type, uint64_t* p) {
+  if ((PyObject*)Py_TYPE(o) != type) return kOther;
+  Py_buffer b;  // the caller holds the structure, and its memory does not move
   if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) < 0) return kError;
   *p = (uint64_t)b.buf;
   PyBuffer_Release(&b);
@@ -113,7 +113,8 @@ PyObject* call_function(PyObject* self, PyObject* const* args, size_t nargsf, Py
     PyObject* o = args[i];
     Taken taken = kPlain;
     switch (f->kinds[i]) {
-      case 'd': taken = descriptor_of(o, &w[n++]); break;
+      case 'd': taken = structure_of(o, g_desc, &w[n++]); break;
+      case 'r': taken = structure_of(o, g_rule, &w[n++]); break;
       case 't':
         if (o == Py_None) w[n] = 0;
         else taken = tensor_of(o, &w[n], nullptr);
@@ -159,7 +160,7 @@ PyObject* make_function(PyObject*, PyObject* args) {
   const size_t n = strlen(kinds);
   size_t words = n;
   for (const char* k = kinds; *k; ++k) words += *k == 'w';
-  if (words > kMaxWords || strspn(kinds, "dtwis") != n) {
+  if (words > kMaxWords || strspn(kinds, "drtwis") != n) {
     PyErr_SetString(PyExc_ValueError, "bad argument kinds");
     return nullptr;
   }
@@ -189,6 +190,14 @@ PyObject* setup(PyObject*, PyObject* args) {
   Py_RETURN_NONE;
 }
 
+// rule(type)
+PyObject* set_rule(PyObject*, PyObject* type) {
+  Py_INCREF(type);
+  Py_XDECREF(g_rule);
+  g_rule = type;
+  Py_RETURN_NONE;
+}
+
 // forked(): this process is a child
 PyObject* forked(PyObject*, PyObject*) {
   g_initialised = false;
@@ -197,6 +206,7 @@ PyObject* forked(PyObject*, PyObject*) {
 
 PyMethodDef g_methods[] = {{"function", make_function, METH_VARARGS, nullptr},
                            {"setup", setup, METH_VARARGS, nullptr},
+                           {"rule", set_rule, METH_O, nullptr},
                            {"forked", forked, METH_NOARGS, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, g_methods};

@@ -1,0 +1,286 @@
+"""The scored router: pins of the oracle's definition, refusals, and the GPU calls against the oracle.
+
+Indices have to be equal.  Gate weights are fp32 values of sums and quotients that are taken in more bits, or in fp32 with fewer than 32
+roundings, so they are within 32 * 2^-24 of the oracle's largest (a token with a share s of a softmax over scores has it from at most
+a subtraction, an exponential of two roundings, a division and a product, and sums of equal signs add their terms' errors).  The gradients'
+terms are products of a few such values and one difference: 64 * 2^-24 of the largest term of a token, which `grad_size` bounds.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import dynmo_oracle as orc
+from paper_2505_14864_amd import binding as B
+
+U = 2.0 ** -24
+
+
+# ---- the oracle's pins -----------------------------------------------------------------------------------------------------
+
+def test_oracle_without_groups_and_bias_is_the_top_k_router():
+    rng = np.random.default_rng(1)
+    lg = rng.standard_normal((50, 16)).astype(np.float32)
+    idx, gate = orc.route_scored(lg, None, 3, "softmax")
+    ref_idx, ref_gate = orc.route_topk(lg, 3)
+    assert np.array_equal(idx, ref_idx)
+    np.testing.assert_allclose(gate, ref_gate, rtol=1e-12)
+    idx, gate = orc.route_scored(lg, None, 3, "softmax", renormalize=False)
+    np.testing.assert_allclose(gate, orc.route_topk_biased(lg, 3, None, "all")[1], rtol=1e-12)
+
+
+def test_oracle_by_hand():
+    # two groups of two; sigmoid scores 0.5, 0.75 | 0.6, 0.2 (logits ln(s / (1 - s)))
+    s = np.array([[0.5, 0.75, 0.6, 0.2]])
+    lg = np.log(s / (1 - s)).astype(np.float32)
+    idx, gate = orc.route_scored(lg, None, 2, "sigmoid", groups=2, top_groups=1, group_best=2, scale=2.0)
+    assert idx.tolist() == [[1, 0]]  # 1.25 against 0.8
+    np.testing.assert_allclose(gate, [[2 * 0.75 / 1.25, 2 * 0.5 / 1.25]], rtol=1e-6)
+    bias = np.array([0, -0.5, 0.3, 0], np.float32)  # order 0.5, 0.25 | 0.9, 0.2
+    idx, gate = orc.route_scored(lg, bias, 2, "sigmoid", groups=2, top_groups=1, group_best=2, renormalize=False)
+    assert idx.tolist() == [[2, 3]]
+    np.testing.assert_allclose(gate, [[0.6, 0.2]], rtol=1e-6)  # the scores, not the order values
+    idx, _ = orc.route_scored(lg, bias, 3, "sigmoid", groups=2, top_groups=2, group_best=1)
+    assert idx.tolist() == [[2, 0, 1]]
+    lg[0, 2] = -np.inf
+    idx, gate = orc.route_scored(lg, bias, 2, "sigmoid", groups=2, top_groups=2, group_best=2)
+    assert idx.tolist() == [[0, 1]]
+    idx, gate = orc.route_scored(np.full((1, 4), np.nan, np.float32), bias, 2, "softmax")
+    assert idx.tolist() == [[-1, -1]] and gate.tolist() == [[0, 0]]
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalize", [False, True])
+def test_oracle_gradient_is_the_difference_quotient(score, renormalize):
+    rng = np.random.default_rng(7)
+    T, E, k = 3, 12, 4
+    z = rng.standard_normal((T, E)).astype(np.float32)
+    idx, _ = orc.route_scored(z, None, k, score, renormalize=renormalize, scale=1.5)
+    dg = rng.standard_normal((T, k))
+
+    def loss(zz):  # the weights of the slots as chosen, in 64 bits
+        p = np.exp(zz - zz.max(1, keepdims=True))
+        s = p / p.sum(1, keepdims=True) if score == "softmax" else 1 / (1 + np.exp(-zz))
+        w = np.take_along_axis(s, idx.astype(np.int64), 1)
+        return float((dg * (w / w.sum(1, keepdims=True) if renormalize else w) * 1.5).sum())
+
+    grad = orc.route_scored_bwd(dg, z, idx, score, renormalize, 1.5)
+    for t in range(T):
+        for e in range(E):
+            h = np.zeros((T, E))
+            h[t, e] = 1e-5
+            diff = (loss(z.astype(np.float64) + h) - loss(z.astype(np.float64) - h)) / 2e-5
+            assert abs(diff - grad[t, e]) < 1e-8, (t, e)
+
+
+# ---- refusals ----------------------------------------------------------------------------------------------------------------
+
+def test_refusals_without_a_gpu():
+    lib, ref = B.lib(), B.C.byref
+
+    def call(E=8, k=2, T=4, dtype="bf16", p=16, **rule):
+        r = B.make_rule(**rule)
+        a = lib.dynmo_route_scored(ref(B.make_desc(T, 8, 8, E, k, dtype)), ref(r), p, None, p, p, None)
+        b = lib.dynmo_route_scored_bwd(ref(B.make_desc(T, 8, 8, E, k, dtype)), ref(r), p, p, p, p, None)
+        assert a == b
+        return a
+
+    assert call(T=0) == 0
+    assert call(p=None) == -1
+    assert call(groups=3, top_groups=1) == -1                 # 8 experts in 3 groups
+    assert call(groups=0) == -1 and call(groups=4, top_groups=0) == -1 and call(groups=4, top_groups=5) == -1
+    assert call(groups=4, top_groups=1, k=3) == -1             # a group has two experts
+    assert call(group_best=0) == -1 and call(group_best=3) == -1
+    assert call(scale=float("inf")) == -1 and call(scale=float("nan")) == -1
+    assert call(E=257) == -2 and call(k=9) == -1
+    assert call(E=256, k=256, T=0) == 0 and call(E=64, k=8, T=0, groups=64, top_groups=8) == 0
+    bad = B.make_rule()
+    bad.score = 2
+    assert lib.dynmo_route_scored(ref(B.make_desc(4, 8, 8, 8, 2, "f32")), ref(bad), 16, None, 16, 16, None) == -1
+    bad.score, bad.renormalize = 0, 2
+    assert lib.dynmo_route_scored(ref(B.make_desc(4, 8, 8, 8, 2, "f32")), ref(bad), 16, None, 16, 16, None) == -1
+    assert lib.dynmo_route_scored(ref(B.make_desc(4, 8, 8, 8, 2, "f32")), None, 16, None, 16, 16, None) == -1
+    with pytest.raises(ValueError):
+        B.make_rule("tanh")
+
+
+class FakeStream:
+    cuda_stream = 0
+
+
+@pytest.mark.parametrize("args", [
+    (B.make_desc(8, 8, 8, 4, 2, "f32"), B.make_desc(8, 8, 8, 4, 2, "f32"), None, None, None, None, FakeStream),
+    (B.make_desc(8, 8, 8, 4, 2, "f32"), None, None, None, None, None, FakeStream),
+    (B.make_rule(), B.make_rule(), None, None, None, None, FakeStream),
+    (B.make_desc(8, 8, 8, 4, 2, "f32"), B.make_rule(), torch.zeros(8), None, None, None, FakeStream),
+    (B.make_desc(8, 8, 8, 4, 2, "f32"), B.make_rule(), None, None, None, None, FakeStream)])
+def test_native_call_takes_what_ctypes_takes(args):
+    name, kinds = "dynmo_route_scored", "drtttts"
+    raised = []
+    for call in (B._calls().function(name, B.C.cast(B.lib().dynmo_route_scored, B.C.c_void_p).value, kinds, B._by_ctypes(name, kinds)),
+                 B._by_ctypes(name, kinds)):
+        with pytest.raises(Exception) as e:
+            call(*args)
+        raised.append((e.type, str(e.value)))
+    assert raised[0] == raised[1]
+
+
+# ---- the GPU ------------------------------------------------------------------------------------------------------------------
+
+def make_logits(kind, T, E, rng):
+    if kind == "normal":
+        return rng.standard_normal((T, E)).astype(np.float32)
+    if kind == "ties":
+        lg = (rng.integers(-2, 3, size=(T, E)) * 0.5).astype(np.float32)
+        lg[::3] = 0.0
+        return lg
+    if kind == "near":  # neighbours one fp32 step apart around large scores, where an fp32 sigmoid cannot tell them apart
+        return (np.float32(9.0) + rng.integers(0, 64, size=(T, E)).astype(np.float32) * np.float32(2.0 ** -20)).astype(np.float32)
+    lg = rng.standard_normal((T, E)).astype(np.float32)  # "masked": -inf, NaN, the lowest value, +inf in places; whole rows of them
+    lg[rng.random((T, E)) < 0.3] = -np.inf
+    lg[rng.random((T, E)) < 0.1] = np.nan
+    lg[rng.random((T, E)) < 0.1] = np.finfo(np.float32).min
+    lg[::5] = -np.inf
+    lg[1::7] = np.nan
+    lg[2::11, : max(1, E // 2)] = np.inf
+    lg[3::13] = np.finfo(np.float32).min
+    return lg
+
+
+def run_route(lg, bias, k, rule, stream=None):
+    T, E = lg.shape
+    d = B.make_desc(T, 8, 8, E, k, "bf16")
+    ei = torch.full((T, k), -7, dtype=torch.int32, device="cuda")
+    gw = torch.full((T, k), -7.0, device="cuda")
+    B.dynmo_route_scored(d, B.make_rule(**rule), torch.from_numpy(lg).cuda(), None if bias is None else torch.from_numpy(bias).cuda(), ei, gw)
+    return ei, gw
+
+
+def check_route(lg, bias, k, rule):
+    ei, gw = run_route(lg, bias, k, rule)
+    idx, gate = orc.route_scored(lg, bias, k, **rule)
+    assert np.array_equal(ei.cpu().numpy(), idx)
+    got = gw.cpu().numpy().astype(np.float64)
+    assert np.isfinite(got).all()
+    assert (np.abs(got - gate) <= 32 * U * np.maximum(np.abs(gate).max(), 1e-30)).all()
+    return idx
+
+
+def check_bwd(lg, idx, k, rule, rng):
+    T, E = lg.shape
+    dg = rng.standard_normal((T, k)).astype(np.float32)
+    out = torch.full((T, E), 7.0, device="cuda")
+    B.dynmo_route_scored_bwd(B.make_desc(T, 8, 8, E, k, "bf16"), B.make_rule(**rule), torch.from_numpy(dg).cuda(), torch.from_numpy(lg).cuda(),
+                             torch.from_numpy(idx).cuda(), out)
+    how = dict(score=rule["score"], renormalize=rule["renormalize"], scale=rule["scale"])
+    ref = orc.route_scored_bwd(dg, lg, idx, **how)
+    # the largest term: ds s, with ds up to |g| / S + |g| s / S^2, and s / S at most 1
+    s, _ = orc.route_scores(lg, rule["score"])
+    grad_size = 2 * np.abs(dg).sum(1) * abs(rule["scale"])
+    if not rule["renormalize"]:
+        grad_size = grad_size * s.max(1)
+    assert (np.abs(out.cpu().numpy() - ref) <= 64 * U * grad_size[:, None] + 1e-37).all()
+
+
+RULES = [dict(score="softmax", groups=1, top_groups=1, group_best=1, renormalize=True, scale=1.0),
+         dict(score="sigmoid", groups=1, top_groups=1, group_best=1, renormalize=True, scale=2.5),
+         dict(score="softmax", groups=1, top_groups=1, group_best=1, renormalize=False, scale=1.0),
+         dict(score="sigmoid", groups=1, top_groups=1, group_best=2, renormalize=False, scale=-0.5)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (7, 2, 1), (100, 3, 2), (257, 5, 5), (333, 8, 2), (130, 16, 4), (65, 33, 7), (64, 64, 64),
+                                   (33, 65, 8), (40, 128, 6), (31, 129, 9), (50, 256, 8), (3, 256, 256), (5, 200, 100)])
+@pytest.mark.parametrize("kind", ["normal", "ties", "near", "masked"])
+def test_route_scored(T, E, k, kind):
+    for i, rule in enumerate(RULES):
+        rng = np.random.default_rng(T * 131 + E * 7 + k + i)
+        lg = make_logits(kind, T, E, rng)
+        bias = None if i % 2 == 0 else (0.1 * rng.standard_normal(E)).astype(np.float32)
+        idx = check_route(lg, bias, k, rule)
+        check_bwd(lg, idx, k, rule, rng)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,E,k,groups,top", [(100, 8, 2, 4, 1), (64, 60, 6, 5, 2), (50, 64, 8, 8, 3), (70, 256, 8, 8, 4), (33, 250, 7, 10, 3),
+                                              (31, 256, 8, 64, 17), (20, 256, 6, 256, 6), (40, 128, 16, 2, 1), (9, 6, 3, 2, 1), (50, 96, 8, 16, 16)])
+@pytest.mark.parametrize("kind", ["normal", "ties", "near", "masked"])
+def test_route_scored_groups(T, E, k, groups, top, kind):
+    for best in (1, 2):
+        for score in ("softmax", "sigmoid"):
+            rng = np.random.default_rng(T * 131 + E * 7 + k + best)
+            lg = make_logits(kind, T, E, rng)
+            bias = None if best == 1 else (0.05 * rng.standard_normal(E)).astype(np.float32)
+            rule = dict(score=score, groups=groups, top_groups=top, group_best=best, renormalize=True, scale=1.0)
+            idx = check_route(lg, bias, k, rule)
+            check_bwd(lg, idx, k, rule, rng)
+
+
+@pytest.mark.gpu
+def test_bias_of_infinities_and_nan():
+    rng = np.random.default_rng(3)
+    lg = rng.standard_normal((70, 24)).astype(np.float32)
+    bias = (0.1 * rng.standard_normal(24)).astype(np.float32)
+    bias[[0, 5, 6, 7, 8, 9, 10, 11]] = [np.nan, -np.inf, np.nan, -np.inf, -np.inf, np.inf, np.inf, -np.inf]
+    for groups, top, best in ((1, 1, 1), (6, 2, 2), (4, 1, 2)):
+        idx = check_route(lg, bias, 4, dict(score="sigmoid", groups=groups, top_groups=top, group_best=best, renormalize=True, scale=1.0))
+        assert not np.isin(idx, [0, 5, 6, 7, 8, 11]).any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_many_tokens_close_to_the_border(score):
+    """A large batch, where some tokens' k-th and next order value differ by less than an fp32 rounding: the indices are still those of the
+    64-bit order.  The reference order is taken by torch in 64 bits."""
+    T, E, k = 65536, 64, 8
+    g = torch.Generator(device="cuda").manual_seed(5)
+    lg = torch.randn((T, E), generator=g, device="cuda")
+    bias = 0.1 * torch.randn(E, generator=g, device="cuda")
+    ei = torch.empty((T, k), dtype=torch.int32, device="cuda")
+    gw = torch.empty((T, k), device="cuda")
+    B.dynmo_route_scored(B.make_desc(T, 8, 8, E, k, "bf16"), B.make_rule(score), lg, bias, ei, gw)
+    s = torch.softmax(lg.double(), -1) if score == "softmax" else torch.sigmoid(lg.double())
+    idx = torch.sort(s + bias.double(), dim=-1, descending=True, stable=True).indices[:, :k]
+    assert torch.equal(ei.long(), idx)
+    w = s.gather(1, idx)
+    assert ((gw.double() - w / w.sum(-1, keepdim=True)).abs() <= 32 * U).all()
+
+
+@pytest.mark.gpu
+def test_backward_of_slots_without_an_expert_and_of_one_expert_twice():
+    rng = np.random.default_rng(9)
+    lg = rng.standard_normal((40, 20)).astype(np.float32)
+    idx = rng.integers(-1, 21, size=(40, 4)).astype(np.int32)  # -1 and 20 are no experts; repeats are likely
+    idx[0], idx[1] = -1, 3
+    for i, rule in enumerate(RULES):
+        check_bwd(lg, idx, 4, rule, rng)
+
+
+@pytest.mark.gpu
+def test_captured_and_on_another_stream():
+    rng = np.random.default_rng(11)
+    lg = rng.standard_normal((300, 48)).astype(np.float32)
+    rule = B.make_rule("sigmoid", groups=4, top_groups=2, group_best=2)
+    d = B.make_desc(300, 8, 8, 48, 4, "bf16")
+    logits = torch.from_numpy(lg).cuda()
+    ei, gw = torch.empty((300, 4), dtype=torch.int32, device="cuda"), torch.empty((300, 4), device="cuda")
+    dl = torch.empty((300, 48), device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        B.dynmo_route_scored(d, rule, logits, None, ei, gw)
+        B.dynmo_route_scored_bwd(d, rule, gw, logits, ei, dl)
+    for seed in range(3):
+        lg = np.random.default_rng(seed).standard_normal((300, 48)).astype(np.float32)
+        logits.copy_(torch.from_numpy(lg))
+        graph.replay()
+        torch.cuda.synchronize()
+        idx, gate = orc.route_scored(lg, None, 4, "sigmoid", 4, 2, 2)
+        assert np.array_equal(ei.cpu().numpy(), idx)
+        ref = orc.route_scored_bwd(gw.cpu().numpy(), lg, idx, "sigmoid")
+        assert np.abs(dl.cpu().numpy() - ref).max() <= 64 * U
+        with torch.cuda.stream(side):
+            e2, g2 = torch.empty_like(ei), torch.empty_like(gw)
+            B.dynmo_route_scored(d, rule, logits, None, e2, g2)
+        side.synchronize()
+        assert torch.equal(e2, ei) and torch.equal(g2, gw)
