@@ -291,6 +291,38 @@ enum {
 };
 int32_t dynmo_grouped_ffn_kernel(const dynmo_desc* d, int32_t product);
 
+/* ---- experts in 4 bits ---------------------------------------------------- */
+
+/* Microscaled 4-bit floating point (the OCP MXFP4 format): a row's values in blocks of 32, a block's values as E2M1 codes (0, 0.5,
+ * 1, 1.5, 2, 3, 4, 6 and their negatives) times one scale 2^(byte - 127).  Quantising, per block: scale = 2^(floor(log2(amax)) - 2)
+ * (at least 2^-127), codes = value / scale to the nearest, ties to the even code, beyond 6 saturated.  A block that holds an
+ * infinity or a NaN becomes NaN as a whole (byte 255).  A last block that K ends inside is as if zeros followed.
+ *
+ * dynmo_mxfp4_bytes: size of one packed matrix [rows, K], a multiple of 256; 0 for rows < 0 or K <= 0.  The packed form is the library's own (codes in
+ * tiles of 16 rows x 128 values in the order in which the matrix cores take them, padded with zeros, then the scales), read and written by these
+ * calls.  Matrices follow one another without gaps: src [n, rows, K] -> packed [n, dynmo_mxfp4_bytes(rows, K)].
+ *
+ * dynmo_mxfp4_quantize: float or bfloat16 -> packed; dynmo_mxfp4_dequantize: packed -> the values it stands for, exact in either
+ * type.  K must be a multiple of 8 (DYNMO_BF16) or 4 (DYNMO_F32), and n * ceil(rows / 16) * ceil(K / 512) below 2^31 (DYNMO_EUNSUPPORTED).
+ * Quantising what dequantising gave returns the same values, so a checkpoint in another order of the same format loses nothing. */
+size_t dynmo_mxfp4_bytes(int32_t rows, int32_t K);
+int32_t dynmo_mxfp4_quantize(int32_t n, int32_t rows, int32_t K, int32_t dtype, const void* src, void* packed, void* stream);
+int32_t dynmo_mxfp4_dequantize(int32_t n, int32_t rows, int32_t K, int32_t dtype, const void* packed, void* dst, void* stream);
+
+size_t dynmo_grouped_ffn_mxfp4_workspace_bytes(const dynmo_desc* d);
+
+/* dynmo_grouped_ffn_fwd on packed weights: with Q the quantisation above, along a row,
+ * G = Q(X) Wg[e]^T, U = Q(X) Wu[e]^T, A = Q(silu(G) * U), Y = A Wd[e]^T; products of 4-bit values on the matrix cores, fp32 sums, G, U and A kept in
+ * fp32 up to A's quantisation.  DYNMO_BF16 only (X, Y and the saved G, U bfloat16), H and F up to 2^22.
+ * src_slot NULL: x is x_p [T*k,H], expert-sorted rows; else x [T,H] in token order, row p being x[src_slot[p] / k] as for
+ * dynmo_grouped_ffn_fwd_gather (of any size).  Wg, Wu [E, dynmo_mxfp4_bytes(F, H)], Wd [E, dynmo_mxfp4_bytes(H, F)].
+ * G_save, U_save [T*k,F]: both, or both NULL.  With them, and with the weights dequantised to bfloat16,
+ * dynmo_grouped_ffn_bwd gives the gradient that passes the quantisations straight through.
+ * A row with an infinity or a NaN gives a row of NaN, other rows do not depend on it.  The workspace holds the quantised X and A. */
+int32_t dynmo_grouped_ffn_mxfp4(const dynmo_desc* d, const void* x, const int32_t* src_slot, const int32_t* seg_offsets, const void* Wg,
+                                const void* Wu, const void* Wd, void* y_p, void* G_save, void* U_save, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
 /* ---- combine ----------------------------------------------------------- */
 
 /* out[t] = base[t] + sum over routed slots s (ascending) of gate_w[t,s] y_p[dst_pos[t,s]].

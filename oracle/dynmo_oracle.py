@@ -339,6 +339,72 @@ def grouped_ffn_fwd(x_p, seg_offsets, Wg, Wu, Wd):
     return y, G, U
 
 
+MXFP4_VALUES = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def mxfp4_quantize(x):
+    """Microscaled 4-bit quantisation (OCP MX format, E2M1 values, E8M0 scales) along the last axis: blocks of 32 (zeros behind the end),
+    scale = 2^(floor(log2(max |x|)) - 2), at least 2^-127; values to the nearest of MXFP4_VALUES, ties to the even code,
+    beyond 6 saturated.  A block with an infinity or a NaN is NaN.
+    Returns the values it stands for (f64, the shape of x), the codes (uint8 0 .. 15, [..., blocks, 32]) and the scale bytes
+    (uint8, [..., blocks]): scale = 2^(byte - 127), 255 for NaN."""
+    x = _f64(x)
+    K = x.shape[-1]
+    blocks = -(-K // 32)
+    b = np.zeros(x.shape[:-1] + (blocks * 32,), F64)
+    b[..., :K] = x
+    b = b.reshape(x.shape[:-1] + (blocks, 32))
+    bad = ~np.isfinite(b).all(-1)
+    clean = np.where(bad[..., None], 0.0, b)
+    amax = np.abs(clean).max(-1)
+    exp = np.where(amax > 0, np.frexp(np.where(amax > 0, amax, 1.0))[1] - 1 - 2, -127)
+    exp = np.maximum(exp, -127)
+    ratio = np.ldexp(np.abs(clean), -exp[..., None])
+    dist = np.abs(ratio[..., None] - MXFP4_VALUES)  # to every value; the even code of the two nearest at a tie
+    near = dist == dist.min(-1, keepdims=True)
+    even = np.arange(8) % 2 == 0
+    code = np.argmax(np.where(near, np.where(even, 2, 1), 0), -1)
+    value = np.ldexp(MXFP4_VALUES[code], exp[..., None]) * np.where(np.signbit(clean), -1.0, 1.0)
+    value = np.where(bad[..., None], np.nan, value).reshape(x.shape[:-1] + (blocks * 32,))[..., :K]
+    code = np.where(bad[..., None], 0, code + 8 * np.signbit(clean)).astype(np.uint8)
+    return value, code, np.where(bad, 255, exp + 127).astype(np.uint8)
+
+
+def mxfp4_pack(codes, scales):
+    """The packed form of one matrix, from its codes [rows, blocks, 32] and scale bytes [rows, blocks], byte by byte: tiles of 16 rows x 128
+    values (1 KB: blocks of 32, of each the 16 rows' 16 bytes, even value in the low half), then the scales (16 rows x 512 values in 256 bytes:
+    block within a tile, row, tile)."""
+    rows, blocks = scales.shape
+    Rb, Kb, Kq = -(-rows // 16), -(-blocks // 4), -(-blocks // 16)
+    code = np.zeros((Rb, Kb, 4, 16, 16), np.uint8)
+    scale = np.zeros((Rb, Kq, 4, 16, 4), np.uint8)
+    for r in range(rows):
+        for b in range(blocks):
+            code[r // 16, b // 4, b % 4, r % 16] = codes[r, b, 0::2] | (codes[r, b, 1::2] << 4)
+            scale[r // 16, b // 16, b % 4, r % 16, b // 4 % 4] = scales[r, b]
+    return np.concatenate([code.ravel(), scale.ravel()])
+
+
+def grouped_ffn_mxfp4(x_p, seg_offsets, Wg, Wu, Wd):
+    """The SwiGLU FFN of grouped_ffn_fwd with its operands quantised along the contraction: rows and A by mxfp4_quantize, the weights given
+    as the values their packed form stands for.  Returns Y, G, U, A before its quantisation."""
+    x_q = mxfp4_quantize(x_p)[0]
+    Wg, Wu, Wd = _f64(Wg), _f64(Wu), _f64(Wd)
+    R = int(seg_offsets[-1])
+    G = np.zeros((R, Wg.shape[1]), F64)
+    U, Y = np.zeros_like(G), np.zeros((R, Wd.shape[1]), F64)
+    for e in range(Wg.shape[0]):
+        rows = slice(int(seg_offsets[e]), int(seg_offsets[e + 1]))
+        G[rows] = x_q[rows] @ Wg[e].T
+        U[rows] = x_q[rows] @ Wu[e].T
+    A = G * _sigmoid(G) * U
+    A_q = mxfp4_quantize(A)[0]
+    for e in range(Wg.shape[0]):
+        rows = slice(int(seg_offsets[e]), int(seg_offsets[e + 1]))
+        Y[rows] = A_q[rows] @ Wd[e].T
+    return Y, G, U, A
+
+
 def grouped_ffn_bwd(dy_p, x_p, G, U, seg_offsets, Wg, Wu, Wd):
     """Backward of grouped_ffn_fwd.
 

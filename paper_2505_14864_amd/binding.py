@@ -74,6 +74,11 @@ SIGNATURES = {
     "dynmo_grouped_ffn_bwd": (_I, [_D] + [_P] * 13 + [C.c_size_t, _P]),
     "dynmo_grouped_ffn_bwd_scatter": (_I, [_D] + [_P] * 16 + [C.c_size_t, _P]),
     "dynmo_grouped_ffn_kernel": (_I, [_D, _I]),
+    "dynmo_mxfp4_bytes": (C.c_size_t, [_I, _I]),
+    "dynmo_mxfp4_quantize": (_I, [_I, _I, _I, _I, _P, _P, _P]),
+    "dynmo_mxfp4_dequantize": (_I, [_I, _I, _I, _I, _P, _P, _P]),
+    "dynmo_grouped_ffn_mxfp4_workspace_bytes": (C.c_size_t, [_D]),
+    "dynmo_grouped_ffn_mxfp4": (_I, [_D] + [_P] * 10 + [C.c_size_t, _P]),
     "dynmo_combine": (_I, [_D, _P, _P, _P, _P, _P, _P]),
     "dynmo_combine_bwd": (_I, [_D, _P, _P, _P, _P, _P, _P, _P]),
     "dynmo_layer_load": (_I, [_D, _P, C.c_double, C.POINTER(C.c_int32), C.POINTER(C.c_double), _P]),
@@ -212,6 +217,7 @@ for _name, _kinds in {
     "dynmo_permute_static": "dtttttts", "dynmo_permute_bwd": "dtttts", "dynmo_grouped_ffn_fwd": "dttttttttws",
     "dynmo_grouped_ffn_fwd_gather": "dtttttttttws", "dynmo_grouped_ffn_fwd_combine": "dtttttttttttttws",
     "dynmo_grouped_ffn_bwd": "dttttttttttttws", "dynmo_grouped_ffn_bwd_scatter": "dtttttttttttttttws",
+    "dynmo_mxfp4_quantize": "iiiitts", "dynmo_mxfp4_dequantize": "iiiitts", "dynmo_grouped_ffn_mxfp4": "dtttttttttws",
     "dynmo_combine": "dttttts", "dynmo_combine_bwd": "dtttttts",
 }.items():
     setattr(_launch, _name, _Launch(_name, _kinds))
@@ -340,6 +346,37 @@ def dynmo_grouped_ffn_kernel(d, product):
     if rc < 0:
         raise DynmoError("dynmo_grouped_ffn_kernel", rc)
     return FFN_KERNELS[rc]
+
+
+def dynmo_mxfp4_bytes(rows, K):
+    return lib().dynmo_mxfp4_bytes(int(rows), int(K))
+
+
+def _mxfp4_sizes(values, packed):
+    """n, rows, K and the type of a tensor [n, rows, K] or [rows, K] whose packed form is `packed`."""
+    code = {torch.float32: DYNMO_F32, torch.bfloat16: DYNMO_BF16}.get(values.dtype)
+    if code is None or values.dim() not in (2, 3) or packed.dtype != torch.uint8:
+        raise ValueError("expected float32 or bfloat16 [n, rows, K] or [rows, K], packed as uint8")
+    n, (rows, K) = values.shape[0] if values.dim() == 3 else 1, values.shape[-2:]
+    if packed.numel() != n * dynmo_mxfp4_bytes(rows, K):
+        raise ValueError("packed holds %d bytes, these matrices take %d" % (packed.numel(), n * dynmo_mxfp4_bytes(rows, K)))
+    return n, rows, K, code
+
+
+def dynmo_mxfp4_quantize(src, packed, stream=None):
+    _launch.dynmo_mxfp4_quantize(*_mxfp4_sizes(src, packed), src, packed, stream)
+
+
+def dynmo_mxfp4_dequantize(packed, dst, stream=None):
+    _launch.dynmo_mxfp4_dequantize(*_mxfp4_sizes(dst, packed), packed, dst, stream)
+
+
+def dynmo_grouped_ffn_mxfp4_workspace_bytes(d):
+    return lib().dynmo_grouped_ffn_mxfp4_workspace_bytes(C.byref(d))
+
+
+def dynmo_grouped_ffn_mxfp4(d, x, src_slot, seg_offsets, Wg, Wu, Wd, y_p, G_save, U_save, workspace, stream=None):
+    _launch.dynmo_grouped_ffn_mxfp4(d, x, src_slot, seg_offsets, Wg, Wu, Wd, y_p, G_save, U_save, workspace, stream)
 
 
 def dynmo_combine(d, y_p, dst_pos, gate_w, base, out, stream=None):

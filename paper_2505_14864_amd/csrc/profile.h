@@ -29,6 +29,8 @@ enum KernelId {
   K_FFN_DWD,
   K_FFN_DWG,
   K_FFN_DWU,
+  K_MXFP4_QUANTIZE,
+  K_MXFP4_DEQUANTIZE,
   K_COUNT
 };
 

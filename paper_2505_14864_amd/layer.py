@@ -3,7 +3,8 @@
 Holds the device buffers of one layer and issues the library calls in order:
   forward : route -> permute -> grouped_ffn_fwd -> combine
             (or permute indices only -> grouped_ffn_fwd_gather -> combine,
-             or, for k = 1, permute -> grouped_ffn_fwd_combine)
+             or, for k = 1, permute -> grouped_ffn_fwd_combine,
+            or, with experts in 4 bits, permute -> grouped_ffn_mxfp4 -> combine)
   backward: combine_bwd -> grouped_ffn_bwd -> permute_bwd -> route_bwd
 Buffers come from torch (device memory only); every step is a library kernel.
 """
@@ -64,6 +65,8 @@ class RoutedFFNLayer:
         self._seg_host = torch.empty(E + 1, dtype=torch.int32, pin_memory=True)
         self._seg_event = torch.cuda.Event()
         self._bwd_ready = False
+        self._rule = None  # of the last route_scored, for route_bwd
+        self._ws_mxfp4 = None
         self._dev = dev
 
     def alloc_backward(self):
@@ -85,7 +88,13 @@ class RoutedFFNLayer:
 
     # ---- routing ----
     def route_topk(self, logits):
+        self._rule = None
         B.dynmo_route_topk(self.d, logits, self.expert_idx, self.gate_w)
+
+    def route_scored(self, logits, rule, bias=None):
+        """Routing by softmax or sigmoid scores (binding.make_rule), `bias` [E] steering the selection."""
+        self._rule = rule
+        B.dynmo_route_scored(self.d, rule, logits, bias, self.expert_idx, self.gate_w)
 
     def route_capacity(self, scores, cap):
         Bn, S = scores.shape
@@ -111,6 +120,21 @@ class RoutedFFNLayer:
         B.dynmo_permute(d, None, self.expert_idx, None, self.seg_offsets, self.src_slot, self.dst_pos, self.ws_permute)
         B.dynmo_grouped_ffn_fwd_gather(d, x, self.src_slot, self.seg_offsets, Wg, Wu, Wd, self.y_p, self.G, self.U,
                                        self.ws_fwd)
+        B.dynmo_combine(d, self.y_p, self.dst_pos, self.gate_w, x if self.residual else None, out)
+        return out
+
+    def forward_mxfp4(self, x, Wg, Wu, Wd, out=None, train=False):
+        """Forward on weights in 4 bits (packed by binding.dynmo_mxfp4_quantize, [E, bytes] each); bf16 layers.  Without `train` the rows are read
+        from x through src_slot and nothing is kept; with it x_p, G and U are, and backward() may follow with the weights
+        dequantised to bf16 (the gradient passes the quantisations straight through)."""
+        d = self.d
+        out = self.out if out is None else out
+        if self._ws_mxfp4 is None:
+            self._ws_mxfp4 = torch.empty((B.dynmo_grouped_ffn_mxfp4_workspace_bytes(d),), dtype=torch.uint8, device=self._dev)
+        B.dynmo_permute(d, x if train else None, self.expert_idx, self.x_p if train else None, self.seg_offsets, self.src_slot, self.dst_pos,
+                        self.ws_permute)
+        B.dynmo_grouped_ffn_mxfp4(d, self.x_p if train else x, None if train else self.src_slot, self.seg_offsets, Wg, Wu, Wd, self.y_p,
+                                  self.G if train else None, self.U if train else None, self._ws_mxfp4)
         B.dynmo_combine(d, self.y_p, self.dst_pos, self.gate_w, x if self.residual else None, out)
         return out
 
@@ -156,8 +180,11 @@ class RoutedFFNLayer:
         return dx
 
     def route_bwd(self, scores=None):
+        """`scores`: what the routing read, where its backward pass needs it (the logits of route_scored, the scores of route_capacity)."""
         self.alloc_backward()
-        if self.mode == "moe":
+        if self._rule is not None:
+            B.dynmo_route_scored_bwd(self.d, self._rule, self.dgate, scores, self.expert_idx, self.droute)
+        elif self.mode == "moe":
             B.dynmo_route_topk_bwd(self.d, self.dgate, self.gate_w, self.expert_idx, self.droute)
         elif self.mode == "mod":
             B.dynmo_route_capacity_bwd(self.d, self.dgate, scores, self.expert_idx, self.droute)

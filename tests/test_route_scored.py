@@ -111,7 +111,7 @@ class FakeStream:
     (B.make_desc(8, 8, 8, 4, 2, "f32"), B.make_desc(8, 8, 8, 4, 2, "f32"), None, None, None, None, FakeStream),
     (B.make_desc(8, 8, 8, 4, 2, "f32"), None, None, None, None, None, FakeStream),
     (B.make_rule(), B.make_rule(), None, None, None, None, FakeStream),
-    (B.make_desc(8, 8, 8, 4, 2, "f32"), B.make_rule(), torch.zeros(8), None, None, None, FakeStream),
+    (B.make_desc(8, 8, 8, 4, 2, "f32"), B.make_rule(), torch.zeros(8, dtype=torch.float32), None, None, None, FakeStream),
     (B.make_desc(8, 8, 8, 4, 2, "f32"), B.make_rule(), None, None, None, None, FakeStream)])
 def test_native_call_takes_what_ctypes_takes(args):
     name, kinds = "dynmo_route_scored", "drtttts"
@@ -150,7 +150,7 @@ def run_route(lg, bias, k, rule, stream=None):
     T, E = lg.shape
     d = B.make_desc(T, 8, 8, E, k, "bf16")
     ei = torch.full((T, k), -7, dtype=torch.int32, device="cuda")
-    gw = torch.full((T, k), -7.0, device="cuda")
+    gw = torch.full((T, k), -7.0, dtype=torch.float32, device="cuda")
     B.dynmo_route_scored(d, B.make_rule(**rule), torch.from_numpy(lg).cuda(), None if bias is None else torch.from_numpy(bias).cuda(), ei, gw)
     return ei, gw
 
@@ -168,7 +168,7 @@ def check_route(lg, bias, k, rule):
 def check_bwd(lg, idx, k, rule, rng):
     T, E = lg.shape
     dg = rng.standard_normal((T, k)).astype(np.float32)
-    out = torch.full((T, E), 7.0, device="cuda")
+    out = torch.full((T, E), 7.0, dtype=torch.float32, device="cuda")
     B.dynmo_route_scored_bwd(B.make_desc(T, 8, 8, E, k, "bf16"), B.make_rule(**rule), torch.from_numpy(dg).cuda(), torch.from_numpy(lg).cuda(),
                              torch.from_numpy(idx).cuda(), out)
     how = dict(score=rule["score"], renormalize=rule["renormalize"], scale=rule["scale"])
@@ -233,10 +233,10 @@ def test_many_tokens_close_to_the_border(score):
     64-bit order.  The reference order is taken by torch in 64 bits."""
     T, E, k = 65536, 64, 8
     g = torch.Generator(device="cuda").manual_seed(5)
-    lg = torch.randn((T, E), generator=g, device="cuda")
-    bias = 0.1 * torch.randn(E, generator=g, device="cuda")
+    lg = torch.randn((T, E), generator=g, dtype=torch.float32, device="cuda")
+    bias = 0.1 * torch.randn(E, generator=g, dtype=torch.float32, device="cuda")
     ei = torch.empty((T, k), dtype=torch.int32, device="cuda")
-    gw = torch.empty((T, k), device="cuda")
+    gw = torch.empty((T, k), dtype=torch.float32, device="cuda")
     B.dynmo_route_scored(B.make_desc(T, 8, 8, E, k, "bf16"), B.make_rule(score), lg, bias, ei, gw)
     s = torch.softmax(lg.double(), -1) if score == "softmax" else torch.sigmoid(lg.double())
     idx = torch.sort(s + bias.double(), dim=-1, descending=True, stable=True).indices[:, :k]
@@ -262,8 +262,8 @@ def test_captured_and_on_another_stream():
     rule = B.make_rule("sigmoid", groups=4, top_groups=2, group_best=2)
     d = B.make_desc(300, 8, 8, 48, 4, "bf16")
     logits = torch.from_numpy(lg).cuda()
-    ei, gw = torch.empty((300, 4), dtype=torch.int32, device="cuda"), torch.empty((300, 4), device="cuda")
-    dl = torch.empty((300, 48), device="cuda")
+    ei, gw = torch.empty((300, 4), dtype=torch.int32, device="cuda"), torch.empty((300, 4), dtype=torch.float32, device="cuda")
+    dl = torch.empty((300, 48), dtype=torch.float32, device="cuda")
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     graph = torch.cuda.CUDAGraph()
