@@ -1,0 +1,92 @@
+// What the kernels of the grouped FFN on MXFP4 weights share (ffn_mxfp4.hip: output tiles, ffn_mxfp4_few.hip: the down product of few rows): a product's
+// parameters, the matrix instruction and the stores of its results.
+#pragma once
+
+#include "ffn_gemm.h"
+#include "mxfp4.h"
+#include "tile_list.h"
+
+namespace dynmo {
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef int v8i __attribute__((ext_vector_type(8)));
+
+struct MxProduct {
+  const int32_t* seg;
+  int E;
+  int N;            // columns of the result: F for gate/up, H for down
+  int K;
+  const char* X;    // the rows: codes, in row blocks of one expert each
+  const char* Xs;   // and their scales
+  const char* W1;   // gate, or down
+  const char* W2;   // up
+  size_t w_bytes;   // of one expert's matrix
+  char* A;          // gate/up: the quantised result (K of the down product = N)
+  char* As;
+  bf16_t* C0;       // down: Y; gate/up: G to save, or nullptr
+  bf16_t* C1;       // U to save, or nullptr
+  TileList list;
+};
+
+// Operand A (16 x 128 4-bit values) is the weights and operand B the rows, so that a lane of the result holds four consecutive columns, 4 (lane /
+// 16) .. + 3, of row lane % 16.  J: which byte of the scale words.
+template <int J>
+__device__ __forceinline__ f32x4_t mx_mfma(v4i a, v4i b, f32x4_t c, int sa, int sb) {
+  const v8i a8 = {a.x, a.y, a.z, a.w, 0, 0, 0, 0}, b8 = {b.x, b.y, b.z, b.w, 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, J, sa, J, sb);
+}
+
+__device__ __forceinline__ uint2 pack_bf16x4(f32x4_t v) { return {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}; }
+
+// 32 columns from n on, a block of the down product's k, of row block rb: silu(G) U quantised and stored, for this lane's row m (one
+// below `m_end`).  The block lies in two results (16 columns each) and four lanes, so its largest value takes two lane exchanges.
+// The logistic function uses the hardware's reciprocal (1 ulp): what follows is a grid of eight steps.
+__device__ __forceinline__ void mx_store_swiglu(const MxProduct& p, const f32x4_t (&g)[2], const f32x4_t (&u)[2], int rb, int m, int m_end, int n) {
+  const int lane = threadIdx.x & 63, quad = lane >> 4, row = lane & 15;
+  const int Fb = mx_k_blocks(p.N), Fq = mx_k_quads(p.N);
+  if (n >= Fb * 128) return;
+  float h[2][4];
+  uint32_t amax = 0;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      h[c][r] = silu_mul(g[c][r], u[c][r]);
+      amax = max(amax, __float_as_uint(h[c][r]) & 0x7fffffffu);
+    }
+    const int col = n + c * 16 + quad * 4;
+    if (p.C0 && m < m_end && col < p.N) {
+      *(uint2*)(p.C0 + (size_t)m * p.N + col) = pack_bf16x4(g[c]);
+      *(uint2*)(p.C1 + (size_t)m * p.N + col) = pack_bf16x4(u[c]);
+    }
+  }
+  amax = max(amax, (uint32_t)__shfl_xor((int)amax, 16, 64));
+  amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32, 64));
+  const uint32_t byte = mx_scale_of(amax);
+  const float scale = mx_scale_value(byte);
+  char* block = p.A + ((size_t)rb * Fb + n / 128) * kMxTile + n % 128 / 32 * 256 + row * 16;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    uint32_t code = 0;
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, h[c][0], h[c][1], scale, 0);
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, h[c][2], h[c][3], scale, 1);
+    *(uint16_t*)(block + c * 8 + quad * 2) = byte == 255 ? (uint16_t)0 : (uint16_t)code;
+  }
+  if (quad == 0) p.As[((size_t)rb * Fq + n / 512) * kMxScales + (n % 128 / 32 * 16 + row) * 4 + n % 512 / 128] = (char)byte;
+}
+
+// Which expert's row block (of 16) or row tile: lane e counts those of expert e, `upto` of the experts up to and with e.
+__device__ __forceinline__ int experts_upto(int count) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(count, d, 64);
+    if (lane >= d) count += o;
+  }
+  return count;
+}
+
+// ffn_mxfp4_few.hip: the down product; at most `max_experts` experts have rows, which are few (right for any number)
+int32_t mx_few_rows(const MxProduct& p, int max_experts, KernelId id, hipStream_t st);
+
+}  // namespace dynmo

@@ -9,40 +9,20 @@
 //
 // One workgroup of four wavefronts (2 x 2) per output tile of 128 weight rows x 128 rows, k in steps of 128 through a ring of three LDS
 // stages; a step's tiles of 1 KB are loaded into LDS as they lie in memory.
-#include "ffn_gemm.h"
-#include "mxfp4.h"
-#include "tile_list.h"
+#include "ffn_mxfp4.h"
 
 namespace dynmo {
 
-typedef int v4i __attribute__((ext_vector_type(4)));
-typedef int v8i __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) v4i lds_v4i;
 typedef __attribute__((address_space(3))) int lds_int;
 
-struct MxProduct {
-  const int32_t* seg;
-  int E;
-  int N;               // columns of the result: F for gate/up, H for down
-  int K;
-  const char* X;       // the rows: codes, in row blocks of one expert each
-  const char* Xs;      // and their scales
-  const char* W1;      // gate, or down
-  const char* W2;      // up
-  size_t w_bytes;      // of one expert's matrix
-  char* A;             // gate/up: the quantised result (K of the down product = N)
-  char* As;
-  bf16_t* C0;          // down: Y; gate/up: G to save, or nullptr
-  bf16_t* C1;          // U to save, or nullptr
-  TileList list;
-};
-
-__device__ __forceinline__ desc_t bytes_desc(const char* p) { return make_desc((const bf16_t*)p, 0x7ffffffeu); }
-
-template <int J>
-__device__ __forceinline__ f32x4_t mx_mfma(v4i a, v4i b, f32x4_t c, int sa, int sb) {
-  const v8i a8 = {a.x, a.y, a.z, a.w, 0, 0, 0, 0}, b8 = {b.x, b.y, b.z, b.w, 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, J, sa, J, sb);
+// load_to_lds() of ffn_gemm.h with a scalar offset, which the bounds check does not see
+template <int LDS_CONST>
+__device__ __forceinline__ void load_to_lds_at(desc_t d, uint32_t lds_base, uint32_t lane_offset, uint32_t offset) {
+  asm volatile("s_add_i32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               :
+               : "s"(lds_base), "v"(lane_offset), "s"(d), "s"(offset), "n"(LDS_CONST)
+               : "memory", "scc");
 }
 
 // BW x BT blocks of 16 x 16 per wavefront, WW x WT wavefronts
@@ -52,10 +32,10 @@ struct MxShape {
   static constexpr int kWaves = WW * WT, kThreads = 64 * kWaves;
   static constexpr int kWBlocks = BW * WW, kTBlocks = BT * WT, kBlocks = kWBlocks + kTBlocks;  // of the tile
   static constexpr int kStages = 3, kAhead = kStages - 1;
-  static constexpr int kStage = kBlocks * kMxTile, kScaleAt = kStages * kStage, kLds = kScaleAt + kBlocks * kMxScales;
-  static constexpr int kLoads = kBlocks / kWaves;               // tiles that a wavefront loads per step
-  static constexpr int kScaleLoads = kBlocks / 4 / kWaves;      // loads of the scales of four steps, 1 KB each
-  static_assert(kBlocks % kWaves == 0 && kBlocks % (4 * kWaves) == 0, "");
+  static constexpr int kLoads = kBlocks / kWaves;                                // tiles that a wavefront loads per step
+  static constexpr int kScaleLoads = (kBlocks / 4 + kWaves - 1) / kWaves;  // loads of the scales of four steps, 1 KB each
+  static constexpr int kStage = kBlocks * kMxTile, kScaleAt = kStages * kStage, kLds = kScaleAt + kScaleLoads * kWaves * 1024;
+  static_assert(kBlocks % kWaves == 0 && kWBlocks % 8 == 0 && kTBlocks % 4 == 0, "the scales of four blocks are loaded together");
   static_assert(kAhead <= 3, "one buffer for the scales: those of the next four steps are loaded after the present ones have been read");
 };
 
@@ -71,12 +51,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void ffn_mx_kernel(const MxProduct 
   const int nt = GATEUP ? (mx_k_blocks(p.N) * 128 + TN - 1) / TN : (p.N + TN - 1) / TN;  // gate/up writes whole tiles of the next k
   const int begin = lane < p.E ? p.seg[lane] : 0, end = lane < p.E ? p.seg[lane + 1] : 0;
   const int mt = (end - begin + TM - 1) / TM, blocks = mx_row_blocks(end - begin);
-  int upto = mt, blocks_upto = blocks;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(upto, d, 64), ob = __shfl_up(blocks_upto, d, 64);
-    if (lane >= d) upto += o, blocks_upto += ob;
-  }
+  const int upto = experts_upto(mt), blocks_upto = experts_upto(blocks);
   const int total = __builtin_amdgcn_readlane(upto, 63) * nt;
   const int pos = list_position(p.list, blockIdx.x, total, TM, S::kWBlocks * 16, p.E, __ballot(mt > 1) == 0);
   const unsigned long long owners = __ballot(upto * nt > pos);
@@ -91,6 +66,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void ffn_mx_kernel(const MxProduct 
   const int t_blocks = min(S::kTBlocks, (m_end - m0 + 15) / 16);
 
   // ---- operands: block b of a step is weight block b (gate/up: the first half gate, the second half the matching up rows) or row block
+  // b - kWBlocks.  A wavefront's loads have a descriptor each, which stays; what changes from step to step is the scalar offset.
   const int Kb = mx_k_blocks(p.K), Kq = mx_k_quads(p.K), Wb = mx_row_blocks(p.N);
   const char* const w1 = p.W1 + e * p.w_bytes;
   const char* const w2 = GATEUP ? p.W2 + e * p.w_bytes : w1;
@@ -98,155 +74,144 @@ __global__ __launch_bounds__(S::kThreads, 2) void ffn_mx_kernel(const MxProduct 
   constexpr int kHalf = GATEUP ? S::kWBlocks / 2 : S::kWBlocks;
   const int nb0 = n0 / 16;
   const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
-  const uint32_t tile_ld = (uint32_t)Kb * kMxTile, scale_ld = (uint32_t)Kq * kMxScales;
-  // where block b of the step lies: its matrix, and its row block there, or -1 where there is none
-  auto place = [&](int b, int* which) {
-    if (b >= S::kWBlocks) {
-      *which = 2;
-      return b - S::kWBlocks < t_blocks ? b - S::kWBlocks : -1;
-    }
-    *which = b >= kHalf ? 1 : 0;
-    const int r = b >= kHalf ? b - kHalf : b;
-    return nb0 + r < Wb ? r : -1;
-  };
-  auto issue = [&](int step, uint32_t stage, auto SCALES) {
-    const bool any = step < Kb;
-    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds0 + stage + wave * S::kLoads * kMxTile);
+  desc_t from[S::kLoads], scales_from[S::kScaleLoads];
+  uint32_t scales_off[S::kScaleLoads];
+  static_for<S::kLoads>([&](auto J) {
+    constexpr int j = decltype(J)::value;
+    const int b = wave * S::kLoads + j, t = b - S::kWBlocks, r = GATEUP && b >= kHalf ? b - kHalf : b;
+    const char* w = (GATEUP && b >= kHalf ? w2 : w1) + (size_t)(nb0 + r) * Kb * kMxTile;
+    const char* x = p.X + (size_t)(rb0 + t) * Kb * kMxTile;
+    from[j] = make_desc((const bf16_t*)(t >= 0 ? x : w), (t >= 0 ? t < t_blocks : nb0 + r < Wb) ? 0x7ffffffeu : 0u);
+  });
+  static_for<S::kScaleLoads>([&](auto J) {
+    constexpr int j = decltype(J)::value;
+    const int b = (wave * S::kScaleLoads + j) * 4, t = b - S::kWBlocks, r = GATEUP && b >= kHalf ? b - kHalf : b;  // four blocks of one matrix
+    const char* w = (GATEUP && b >= kHalf ? w2 : w1) + scales_at + (size_t)(nb0 + r) * Kq * kMxScales;
+    const char* x = p.Xs + (size_t)(rb0 + t) * Kq * kMxScales;
+    scales_from[j] = make_desc((const bf16_t*)(t >= 0 ? x : w), 0x7ffffffeu);
+    const int q = lane >> 4;
+    scales_off[j] = (t >= 0 ? t + q < t_blocks : nb0 + r + q < Wb) ? (uint32_t)q * (uint32_t)Kq * kMxScales + (lane & 15) * 16 : kOob;
+  });
+  const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + wave * S::kLoads * kMxTile);
+  const uint32_t scales_to = __builtin_amdgcn_readfirstlane(lds0 + S::kScaleAt + wave * S::kScaleLoads * 1024);
+  auto issue = [&](int step, uint32_t stage, auto SCALES) {  // past the last step the loads fetch nothing
+    const uint32_t off = step < Kb ? lane * 16 : kOob;
     static_for<S::kLoads>([&](auto J) {
       constexpr int j = decltype(J)::value;
-      int which;
-      const int r = place(wave * S::kLoads + j, &which);
-      const char* base = which == 2 ? p.X + ((size_t)rb0 * Kb + step) * kMxTile : (which == 1 ? w2 : w1) + ((size_t)nb0 * Kb + step) * kMxTile;
-      load_to_lds<j * kMxTile>(bytes_desc(base), lds, any && r >= 0 ? (uint32_t)r * tile_ld + lane * 16 : kOob);
+      load_to_lds_at<j * kMxTile>(from[j], to + stage, off, (uint32_t)step * kMxTile);
     });
     if constexpr (decltype(SCALES)::value) {
-      const int kq = step / 4;
-      const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + S::kScaleAt + wave * S::kScaleLoads * 1024);
       static_for<S::kScaleLoads>([&](auto J) {
         constexpr int j = decltype(J)::value;
-        int which;  // the four blocks of a load lie in one matrix
-        const int b = (wave * S::kScaleLoads + j) * 4;
-        place(b, &which);
-        int unused;
-        const int r = place(b + (lane >> 4), &unused);
-        const char* base = which == 2 ? p.Xs + ((size_t)rb0 * Kq + kq) * kMxScales : (which == 1 ? w2 : w1) + scales_at + ((size_t)nb0 * Kq + kq) * kMxScales;
-        load_to_lds<j * 1024>(bytes_desc(base), to, any && r >= 0 ? (uint32_t)r * scale_ld + (lane & 15) * 16 : kOob);
+        load_to_lds_at<j * 1024>(scales_from[j], scales_to, step < Kb ? scales_off[j] : kOob, (uint32_t)(step / 4) * kMxScales);
       });
     }
   };
 
   const int my_blocks = max(0, min(BT, (t_blocks - wt + WT - 1) / WT));  // row blocks wt, wt + WT, .. of the tile
-  auto w_block = [&](int i) { return GATEUP ? (i < BW / 2 ? ww * (BW / 2) + i : kHalf + ww * (BW / 2) + i - BW / 2) : ww * BW + i; };
-  auto t_block = [&](int i) { return S::kWBlocks + wt + WT * i; };
+  // the first of this wavefront's weight blocks (gate/up: gate blocks, then the up blocks kHalf further on), and of its row blocks
+  const int w_first = GATEUP ? ww * (BW / 2) : ww * BW, t_first = S::kWBlocks + wt;
+  constexpr auto w_place = [](int i) { return GATEUP && i >= BW / 2 ? kHalf + i - BW / 2 : i; };
+  const uint32_t w_at = lds0 + w_first * kMxTile + lane * 16, t_at = lds0 + t_first * kMxTile + lane * 16;
+  const uint32_t sw_at = lds0 + S::kScaleAt + w_first * kMxScales + lane * 4, st_at = lds0 + S::kScaleAt + t_first * kMxScales + lane * 4;
 
   f32x4_t acc[BW][BT] = {};
   static_for<S::kAhead>([&](auto J) {
     constexpr int j = decltype(J)::value;
     issue(j, j * S::kStage, std::integral_constant<bool, j % 4 == 0>{});
   });
-  int sw[BW], sx[BT];
-  uint32_t stage = 0, freed = S::kAhead * S::kStage;
-  for (int kt = 0; kt < Kb; kt += 4) {
-    static_for<4>([&](auto J) {
-      constexpr int j = decltype(J)::value;
-      if (kt + j < Kb) {
-        // this wavefront's share of the stage has landed and its reads of the previous stage are done; behind the barrier
-        // that holds for all.  Loads of the steps j + 1 .. j + kAhead - 1 may still be on their way.
-        constexpr int scales = ((j + 1) % 4 == 0 && S::kAhead > 1) + ((j + 2) % 4 == 0 && S::kAhead > 2);
-        wait_stage<(S::kAhead - 1) * S::kLoads + scales * S::kScaleLoads>();
-        __builtin_amdgcn_s_barrier();
-        issue(kt + j + S::kAhead, freed, std::integral_constant<bool, (j + S::kAhead) % 4 == 0>{});
-        if (j == 0) {
+  auto loop = [&](auto ROWS_C) {
+    constexpr int ROWS = decltype(ROWS_C)::value;
+    int sw[BW], sx[BT];
+    uint32_t stage = 0, freed = S::kAhead * S::kStage;  // the stage read, the stage filled
+    for (int kt = 0; kt < Kb; kt += 4) {
+      static_for<4>([&](auto J) {
+        constexpr int j = decltype(J)::value;
+        if (kt + j < Kb) {
+          // this wavefront's share of the stage has landed and its reads of the previous stage are done; behind the barrier
+          // that holds for all.  Loads of the steps j + 1 .. j + kAhead - 1 may still be on their way.
+          constexpr int scales = ((j + 1) % 4 == 0 && S::kAhead > 1) + ((j + 2) % 4 == 0 && S::kAhead > 2);
+          wait_stage<(S::kAhead - 1) * S::kLoads + scales * S::kScaleLoads>();
+          __builtin_amdgcn_s_barrier();
+          issue(kt + j + S::kAhead, freed, std::integral_constant<bool, (j + S::kAhead) % 4 == 0>{});
+          if constexpr (ROWS > 0) {
+            if constexpr (j == 0) {
 #pragma unroll
-          for (int i = 0; i < BW; ++i) sw[i] = *(const lds_int*)(uintptr_t)(lds0 + S::kScaleAt + w_block(i) * kMxScales + lane * 4);
+              for (int i = 0; i < BW; ++i) sw[i] = *(const lds_int*)(uintptr_t)(sw_at + w_place(i) * kMxScales);
 #pragma unroll
-          for (int i = 0; i < BT; ++i) sx[i] = *(const lds_int*)(uintptr_t)(lds0 + S::kScaleAt + t_block(i) * kMxScales + lane * 4);
+              for (int i = 0; i < ROWS; ++i) sx[i] = *(const lds_int*)(uintptr_t)(st_at + WT * i * kMxScales);
+            }
+            v4i w[BW], x[BT];
+#pragma unroll
+            for (int i = 0; i < BW; ++i) w[i] = *(const lds_v4i*)(uintptr_t)(w_at + stage + w_place(i) * kMxTile);
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) x[i] = *(const lds_v4i*)(uintptr_t)(t_at + stage + WT * i * kMxTile);
+#pragma unroll
+            for (int b = 0; b < ROWS; ++b)
+#pragma unroll
+              for (int a = 0; a < BW; ++a) acc[a][b] = mx_mfma<j>(w[a], x[b], acc[a][b], sw[a], sx[b]);
+          }
+          freed = stage;
+          stage = stage + S::kStage == S::kScaleAt ? 0 : stage + S::kStage;
         }
-        if (my_blocks > 0) {
-          v4i w[BW], x[BT];
-#pragma unroll
-          for (int i = 0; i < BW; ++i) w[i] = *(const lds_v4i*)(uintptr_t)(lds0 + stage + w_block(i) * kMxTile + lane * 16);
-#pragma unroll
-          for (int i = 0; i < BT; ++i) x[i] = *(const lds_v4i*)(uintptr_t)(lds0 + stage + t_block(i) * kMxTile + lane * 16);
-#pragma unroll
-          for (int b = 0; b < BT; ++b)
-#pragma unroll
-            for (int a = 0; a < BW; ++a) acc[a][b] = mx_mfma<j>(w[a], x[b], acc[a][b], sw[a], sx[b]);
-        }
-        freed = stage;
-        stage = stage + S::kStage == S::kScaleAt ? 0 : stage + S::kStage;
-      }
-    });
-  }
+      });
+    }
+  };
+  if (my_blocks == 0) loop(std::integral_constant<int, 0>{});
+  else if (my_blocks <= BT / 4) loop(std::integral_constant<int, BT / 4>{});
+  else if (my_blocks <= BT / 2) loop(std::integral_constant<int, BT / 2>{});
+  else if (my_blocks <= BT * 3 / 4) loop(std::integral_constant<int, BT * 3 / 4>{});
+  else loop(std::integral_constant<int, BT>{});
   wait_stage<0>();  // every load (masked ones included) has landed
 
-  // ---- epilogue.  Element r of block (a, b): column 16 a + 4 (lane / 16) + r, row lane % 16 of row block b.
-  const int g = lane >> 4, row = lane & 15;
+  // ---- epilogue
+  const int row = lane & 15;
 #pragma unroll
   for (int b = 0; b < BT; ++b) {
     if (b >= my_blocks) break;
     const int tb = wt + WT * b, m = m0 + tb * 16 + row;
     if constexpr (GATEUP) {
-      const int Fb = mx_k_blocks(p.N), Fq = mx_k_quads(p.N);
 #pragma unroll
-      for (int a = 0; a < BW / 2; a += 2) {  // two blocks are 32 columns: a block of the next product's k
-        const int n = n0 + (ww * (BW / 2) + a) * 16;
-        float h[2][4];
-        uint32_t amax = 0;
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int col = n + c * 16 + g * 4;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float gv = acc[a + c][b][r], uv = acc[BW / 2 + a + c][b][r];
-            h[c][r] = gv / (1.f + __expf(-gv)) * uv;
-            amax = max(amax, __float_as_uint(h[c][r]) & 0x7fffffffu);
-          }
-          if (p.C0 && m < m_end && col < p.N) {
-            const uint2 gs = {pack_bf16x2(acc[a + c][b][0], acc[a + c][b][1]), pack_bf16x2(acc[a + c][b][2], acc[a + c][b][3])};
-            const f32x4_t u4 = acc[BW / 2 + a + c][b];
-            const uint2 us = {pack_bf16x2(u4[0], u4[1]), pack_bf16x2(u4[2], u4[3])};
-            *(uint2*)(p.C0 + (size_t)m * p.N + col) = gs;
-            *(uint2*)(p.C1 + (size_t)m * p.N + col) = us;
-          }
-        }
-        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 16, 64));
-        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32, 64));
-        const uint32_t byte = mx_scale_of(amax);
-        const float scale = mx_scale_value(byte);
-        if (n >= Fb * 128) continue;
-        char* block = p.A + ((size_t)(rb0 + tb) * Fb + n / 128) * kMxTile + n % 128 / 32 * 256 + row * 16;
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint32_t code = 0;
-          code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, h[c][0], h[c][1], scale, 0);
-          code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, h[c][2], h[c][3], scale, 1);
-          *(uint16_t*)(block + c * 8 + g * 2) = byte == 255 ? (uint16_t)0 : (uint16_t)code;
-        }
-        if (g == 0) p.As[((size_t)(rb0 + tb) * Fq + n / 512) * kMxScales + (n % 128 / 32 * 16 + row) * 4 + n % 512 / 128] = (char)byte;
+      for (int a = 0; a < BW / 2; a += 2) {
+        const f32x4_t g2[2] = {acc[a][b], acc[a + 1][b]}, u2[2] = {acc[BW / 2 + a][b], acc[BW / 2 + a + 1][b]};
+        mx_store_swiglu(p, g2, u2, rb0 + tb, m, m_end, n0 + (ww * (BW / 2) + a) * 16);
       }
     } else {
 #pragma unroll
       for (int a = 0; a < BW; ++a) {
-        const int col = n0 + (ww * BW + a) * 16 + g * 4;
-        if (m >= m_end || col >= p.N) continue;
-        const uint2 y = {pack_bf16x2(acc[a][b][0], acc[a][b][1]), pack_bf16x2(acc[a][b][2], acc[a][b][3])};
-        *(uint2*)(p.C0 + (size_t)m * p.N + col) = y;
+        const int col = n0 + (ww * BW + a) * 16 + (lane >> 4) * 4;
+        if (m < m_end && col < p.N) *(uint2*)(p.C0 + (size_t)m * p.N + col) = pack_bf16x4(acc[a][b]);
       }
     }
   }
 }
 
 template <bool GATEUP, class S>
-static int32_t launch_mx(MxProduct p, const dynmo_desc* d, KernelId id, hipStream_t st) {
+static int64_t mx_tile_count(const MxProduct& p, const dynmo_desc* d) {
   constexpr int TN = S::kWBlocks * 16 / (GATEUP ? 2 : 1), TM = S::kTBlocks * 16;
   const int64_t rows = (int64_t)d->T * d->k, row_tiles = rows / TM + (rows < d->E ? rows : d->E);
-  const int64_t tiles = row_tiles * (((GATEUP ? (int64_t)mx_k_blocks(p.N) * 128 : p.N) + TN - 1) / TN);
+  return row_tiles * (((GATEUP ? (int64_t)mx_k_blocks(p.N) * 128 : p.N) + TN - 1) / TN);
+}
+
+template <bool GATEUP, class S>
+static int32_t launch_mx(MxProduct p, const dynmo_desc* d, KernelId id, hipStream_t st) {
+  const int64_t tiles = mx_tile_count<GATEUP, S>(p, d);
   if (tiles == 0) return DYNMO_OK;
   if (tiles > (1 << 30)) return DYNMO_EUNSUPPORTED;
   p.list = tile_list((int)tiles);
   DYNMO_TIMED_LAUNCH(id, st, ffn_mx_kernel<GATEUP, S><<<dim3(p.list.blocks), dim3(S::kThreads), 0, st>>>(p));
   return DYNMO_OK;
+}
+
+// Tiles of 256 weight rows where they fill the chip four times over (two workgroups on each of 256 compute units), of 128 (three) else.
+// Both, us: 8 experts, 8192 rows, 4096 x 14336, gate/up (8064 tiles of 256) 602 / 636, down 316 / 313; 2000 rows, gate/up (2688) 163 / 168,
+// down (400) 116 / 112; 16 experts, 32768 rows, 4096 x 688, gate/up (1664) 130 / 127, down (4352) 146 / 153; 8 experts, 2048 rows,
+// 2048 x 4096, gate/up (768) 39 / 33.
+template <bool GATEUP>
+static int32_t mx_tiles(const MxProduct& p, const dynmo_desc* d, KernelId id, hipStream_t st) {
+  using Wide = MxShape<8, 4, 2, 2>;
+  if (mx_tile_count<GATEUP, Wide>(p, d) >= 4 * 512) return launch_mx<GATEUP, Wide>(p, d, id, st);
+  return launch_mx<GATEUP, MxShape<4, 4, 2, 2>>(p, d, id, st);
 }
 
 struct MxWorkspace {
@@ -301,7 +266,7 @@ extern "C" int32_t dynmo_grouped_ffn_mxfp4(const dynmo_desc* d, const void* x, c
   p.As = base + w.as;
   p.C0 = (bf16_t*)G_save;
   p.C1 = (bf16_t*)U_save;
-  r = launch_mx<true, MxShape<4, 4, 2, 2>>(p, d, K_FFN_GATEUP, st);
+  r = mx_tiles<true>(p, d, K_FFN_GATEUP, st);
   if (r) return r;
   p.N = d->H;
   p.K = d->F;
@@ -310,5 +275,10 @@ extern "C" int32_t dynmo_grouped_ffn_mxfp4(const dynmo_desc* d, const void* x, c
   p.W1 = (const char*)Wd;
   p.w_bytes = mx_bytes(d->H, d->F);
   p.C0 = (bf16_t*)y_p;
-  return launch_mx<false, MxShape<4, 4, 2, 2>>(p, d, K_FFN_DOWN, st);
+  // Up to 64 tokens and as many tiles as compute units the weights are read faster without tiles (figures in ffn_mxfp4_few.hip; beyond: 64
+  // experts, 512 rows, 2048 x 1024, 1024 tiles, 20 us against 17.5; 8 experts, 256 rows, 4096 x 14336 57 against 52).
+  const int64_t rows = (int64_t)d->T * d->k;
+  const int max_experts = (int)(rows < d->E ? rows : d->E);
+  if (d->T <= 64 && (int64_t)max_experts * ((d->H + 127) / 128) <= 256) return mx_few_rows(p, max_experts, K_FFN_DOWN, st);
+  return mx_tiles<false>(p, d, K_FFN_DOWN, st);
 }

@@ -1,67 +1,92 @@
 // MXFP4 quantisation and its reverse.  Bound by memory: a value is read once and 17/32 byte written (or the other way round).
-#include "mxfp4.h"
+#include "ffn_mxfp4.h"
 
 #include "profile.h"
 
 namespace dynmo {
 
-// One workgroup: 16 rows x 512 values, a wavefront for each tile of 128.  Four lanes hold a block of 32 (eight values each), sixteen
-// lanes a row, so that a wavefront reads 256 (fp32: 512) contiguous bytes of four rows at a time; the scales of the four tiles meet in LDS.
-constexpr int kQuantThreads = 256;
+// A wavefront takes tiles of 16 rows x 128 values, one after another along a row block, and asks for the next one before it works on the
+// present one.  Four lanes hold a block of 32 (eight values each), sixteen lanes a row, so that a load of the wavefront covers 256 (fp32: 512)
+// contiguous bytes of four rows, and a store 64 bytes of each block column.  The four wavefronts of a workgroup share a row block.
+constexpr int kQuantThreads = 256, kQuantWaves = 4;
 
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, int left, float* v) {
+__device__ __forceinline__ void load8(const T* p, int left, u32x4* v) {
   constexpr int kVec = Elem<T>::kVec;
 #pragma unroll
-  for (int i = 0; i < 8; i += kVec) {
-    const u32x4 zero = {0u, 0u, 0u, 0u};
-    unpack16<T>(i < left ? *(const u32x4*)(p + i) : zero, v + i);
+  for (int i = 0; i < 8 / kVec; ++i) {
+    v[i] = u32x4{0u, 0u, 0u, 0u};
+    if (i * kVec < left) v[i] = *(const u32x4*)(p + i * kVec);
   }
 }
+
+// the value of lane ^ 1, lane ^ 2
+__device__ __forceinline__ uint32_t quad_xor1(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true); }
+__device__ __forceinline__ uint32_t quad_xor2(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true); }
 
 // Eight values of each lane -> their codes, and the block's scale byte (the same in the four lanes of a block)
 __device__ __forceinline__ uint32_t quantize_block(const float* v, uint32_t* scale) {
   uint32_t amax = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(v[i]) & 0x7fffffffu);
-  amax = max(amax, (uint32_t)__shfl_xor((int)amax, 1, 64));
-  amax = max(amax, (uint32_t)__shfl_xor((int)amax, 2, 64));
+  amax = max(amax, quad_xor1(amax));
+  amax = max(amax, quad_xor2(amax));
   *scale = mx_scale_of(amax);
   return *scale == 255 ? 0u : mx_codes8(v, mx_scale_value(*scale));
 }
 
-// `row(r)`: the source row of row r (0 .. 15) of the block, or nullptr
-template <typename T, typename Row>
-__device__ __forceinline__ void quantize_rows(Row&& row, int K, int kq, int Kb, char* codes, char* scales) {
-  __shared__ uint32_t quad[64];
-  const int lane = threadIdx.x & 63, tile = threadIdx.x >> 6, kb = kq * 4 + tile;
-  const int k = kb * 128 + (lane & 15) * 8, g = (lane & 15) >> 2;
+// Tiles first, first + stride, .. of a row block.  src[i]: this lane's row 4 i + lane / 16 of it, or nullptr.
+template <typename T>
+__device__ __forceinline__ void quantize_rows(const T* const (&src)[4], int K, int first, int stride, char* codes, char* scales) {
+  constexpr int kPieces = 8 / Elem<T>::kVec;
+  const int lane = threadIdx.x & 63, g = (lane & 15) >> 2, Kb = mx_k_blocks(K), tiles = mx_k_quads(K) * 4;
+  u32x4 next[4][kPieces];
+  auto load = [&](int kb) {
+    const int k = kb * 128 + (lane & 15) * 8;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = 4 * i + (lane >> 4);
-    const T* src = row(r);
-    float v[8];
-    load8<T>(src + k, src ? K - k : 0, v);
-    uint32_t scale;
-    const uint32_t c = quantize_block(v, &scale);
-    if (kb < Kb) *(uint32_t*)(codes + (size_t)kb * kMxTile + g * 256 + r * 16 + (lane & 3) * 4) = c;
-    if ((lane & 3) == 0) ((uint8_t*)quad)[(g * 16 + r) * 4 + tile] = (uint8_t)scale;
+    for (int i = 0; i < 4; ++i) load8<T>(src[i] + k, src[i] ? K - k : 0, next[i]);
+  };
+  load(first);
+  for (int kb = first; kb < tiles; kb += stride) {  // tiles from Kb on have scales (zero) only
+    u32x4 now[4][kPieces];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < kPieces; ++c) now[i][c] = next[i][c];
+    if (kb + stride < Kb) load(kb + stride);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 4 * i + (lane >> 4);
+      uint32_t scale = 0;
+      if (kb < Kb) {
+        float v[8];
+#pragma unroll
+        for (int c = 0; c < kPieces; ++c) unpack16<T>(now[i][c], v + c * Elem<T>::kVec);
+        *(uint32_t*)(codes + (size_t)kb * kMxTile + g * 256 + r * 16 + (lane & 3) * 4) = quantize_block(v, &scale);
+      }
+      if ((lane & 3) == 0) scales[(size_t)(kb / 4) * kMxScales + (g * 16 + r) * 4 + kb % 4] = (char)scale;
+    }
   }
-  __syncthreads();
-  if (threadIdx.x < 64) *(uint32_t*)(scales + (size_t)kq * kMxScales + lane * 4) = quad[lane];
 }
 
 template <typename T>
-__global__ __launch_bounds__(kQuantThreads) void mx_quantize_kernel(const T* __restrict__ src, char* __restrict__ packed, int rows, int K) {
+__global__ __launch_bounds__(kQuantThreads) void mx_quantize_kernel(const T* __restrict__ src, char* __restrict__ packed, int rows, int K, int parts) {
   const int Kb = mx_k_blocks(K), Kq = mx_k_quads(K), Rb = mx_row_blocks(rows);
-  const unsigned kq = blockIdx.x % Kq, at = blockIdx.x / Kq;
-  const int rb = at % Rb;
+  const unsigned part = blockIdx.x % parts, at = blockIdx.x / parts;
+  const int rb = at % Rb, lane = threadIdx.x & 63;
   const long m = at / Rb;
   char* matrix = packed + m * mx_bytes(rows, K);
-  quantize_rows<T>([&](int r) { return rb * 16 + r < rows ? src + (m * rows + rb * 16 + r) * (long)K : nullptr; }, K, kq, Kb,
-                   matrix + (size_t)rb * Kb * kMxTile, matrix + mx_code_bytes(Rb, K) + (size_t)rb * Kq * kMxScales);
+  const T* row[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = rb * 16 + 4 * i + (lane >> 4);
+    row[i] = r < rows ? src + (m * rows + r) * (long)K : nullptr;
+  }
+  quantize_rows<T>(row, K, part * kQuantWaves + (threadIdx.x >> 6), parts * kQuantWaves, matrix + (size_t)rb * Kb * kMxTile,
+                   matrix + mx_code_bytes(Rb, K) + (size_t)rb * Kq * kMxScales);
 }
 
+// Values four at a time: a store of the wavefront covers the 128 values of two rows (fp32: 512 contiguous bytes each).
 template <typename T>
 __global__ __launch_bounds__(kQuantThreads) void mx_dequantize_kernel(const char* __restrict__ packed, T* __restrict__ dst, int rows, int K) {
   const int Kb = mx_k_blocks(K), Kq = mx_k_quads(K), Rb = mx_row_blocks(rows);
@@ -69,71 +94,68 @@ __global__ __launch_bounds__(kQuantThreads) void mx_dequantize_kernel(const char
   const int rb = at % Rb;
   const long m = at / Rb;
   const char* matrix = packed + m * mx_bytes(rows, K);
-  const char* codes = matrix + (size_t)rb * Kb * kMxTile;
-  const char* scales = matrix + mx_code_bytes(Rb, K) + ((size_t)rb * Kq + kq) * kMxScales;
   const int lane = threadIdx.x & 63, tile = threadIdx.x >> 6, kb = kq * 4 + tile;
-  const int k = kb * 128 + (lane & 15) * 8, g = (lane & 15) >> 2;
+  const int c0 = (lane & 31) * 4, k = kb * 128 + c0, g = c0 / 32;
   if (k >= K) return;
+  const char* codes = matrix + ((size_t)rb * Kb + kb) * kMxTile + g * 256 + c0 % 32 / 2;
+  const char* scales = matrix + mx_code_bytes(Rb, K) + ((size_t)rb * Kq + kq) * kMxScales + g * 64 + tile;
+  uint32_t code[8], byte[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = 4 * i + (lane >> 4);
-    if (rb * 16 + r >= rows) break;
-    const uint32_t c = *(const uint32_t*)(codes + (size_t)kb * kMxTile + g * 256 + r * 16 + (lane & 3) * 4);
-    const uint32_t byte = ((const uint8_t*)scales)[(g * 16 + r) * 4 + tile];
-    const float scale = mx_scale_value(byte);
-    float v[8];
-    f32x2_t two;
-    two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 0), v[0] = two.x, v[1] = two.y;
-    two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 1), v[2] = two.x, v[3] = two.y;
-    two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 2), v[4] = two.x, v[5] = two.y;
-    two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 3), v[6] = two.x, v[7] = two.y;
-    if (byte == 255)
+  for (int i = 0; i < 8; ++i) {  // behind the last row there are zeros
+    code[i] = *(const uint16_t*)(codes + (2 * i + (lane >> 5)) * 16);
+    byte[i] = *(const uint8_t*)(scales + (2 * i + (lane >> 5)) * 4);
+  }
 #pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] = __uint_as_float(0x7fc00000u);
-    T* to = dst + (m * rows + rb * 16 + r) * (long)K + k;
-    constexpr int kVec = Elem<T>::kVec;
-#pragma unroll
-    for (int q = 0; q < 8; q += kVec)
-      if (k + q < K) *(u32x4*)(to + q) = pack16<T>(v + q);
+  for (int i = 0; i < 8; ++i) {
+    const int r = rb * 16 + 2 * i + (lane >> 5);
+    if (r >= rows) break;
+    const float scale = mx_scale_value(byte[i]);
+    f32x2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[i], scale, 0), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[i], scale, 1);
+    if (byte[i] == 255) lo.x = lo.y = hi.x = hi.y = __uint_as_float(0x7fc00000u);
+    T* to = dst + (m * rows + r) * (long)K + k;
+    if constexpr (sizeof(T) == 2) *(uint2*)to = uint2{pack_bf16x2(lo.x, lo.y), pack_bf16x2(hi.x, hi.y)};
+    else *(u32x4*)to = u32x4{__float_as_uint(lo.x), __float_as_uint(lo.y), __float_as_uint(hi.x), __float_as_uint(hi.y)};
   }
 }
 
 template <typename T>
 __global__ __launch_bounds__(kQuantThreads) void mx_quantize_segments_kernel(const T* __restrict__ x, const int32_t* __restrict__ gather,
-                                                                             int gather_div, const int32_t* __restrict__ seg, int E, int K,
+                                                                             int gather_div, const int32_t* __restrict__ seg, int E, int K, int parts,
                                                                              char* __restrict__ codes, char* __restrict__ scales) {
   const int Kb = mx_k_blocks(K), Kq = mx_k_quads(K);
-  const int kq = blockIdx.x % (unsigned)Kq, rb = blockIdx.x / (unsigned)Kq;
+  const int part = blockIdx.x % (unsigned)parts, rb = blockIdx.x / (unsigned)parts;
   // lane e counts the row blocks of expert e; a prefix sum and a ballot find the owner of block rb
   const int lane = threadIdx.x & 63;
   const int begin = lane < E ? seg[lane] : 0, end = lane < E ? seg[lane + 1] : 0;
-  const int blocks = mx_row_blocks(end - begin);
-  int upto = blocks;
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const int o = __shfl_up(upto, m, 64);
-    if (lane >= m) upto += o;
-  }
+  const int blocks = mx_row_blocks(end - begin), upto = experts_upto(blocks);
   const unsigned long long owners = __ballot(upto > rb);
   if (owners == 0) return;
   const int e = __builtin_ctzll(owners);
   const int first = __builtin_amdgcn_readlane(begin, e) + (rb - (__builtin_amdgcn_readlane(upto, e) - __builtin_amdgcn_readlane(blocks, e))) * 16;
   const int last = __builtin_amdgcn_readlane(end, e);
-  quantize_rows<T>(
-      [&](int r) -> const T* {
-        if (first + r >= last) return nullptr;
-        return x + (long)(gather ? gather[first + r] / gather_div : first + r) * K;
-      },
-      K, kq, Kb, codes + (size_t)rb * Kb * kMxTile, scales + (size_t)rb * Kq * kMxScales);
+  const T* row[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int p = first + 4 * i + (lane >> 4);
+    row[i] = p < last ? x + (size_t)(gather ? gather[p] / gather_div : p) * K : nullptr;
+  }
+  quantize_rows<T>(row, K, part * kQuantWaves + (threadIdx.x >> 6), parts * kQuantWaves, codes + (size_t)rb * Kb * kMxTile,
+                   scales + (size_t)rb * Kq * kMxScales);
+}
+
+// Workgroups per row block: as many as the block has tiles for, but no more than some eight per compute unit in all.
+static int parts_of(int64_t row_blocks, int K) {
+  const int64_t most = mx_k_quads(K), some = (2048 + row_blocks - 1) / (row_blocks > 0 ? row_blocks : 1);
+  return (int)(some < most ? some : most);
 }
 
 int32_t mx_quantize_segments(const dynmo_desc* d, const void* x, const int32_t* gather, const int32_t* seg, int K, void* codes, void* scales,
                              hipStream_t st) {
-  const int64_t blocks = mx_max_row_blocks(d) * mx_k_quads(K);
-  if (blocks == 0) return DYNMO_OK;
-  if (blocks > 0x7fffffff) return DYNMO_EUNSUPPORTED;
-  DYNMO_TIMED_LAUNCH(K_MXFP4_QUANTIZE, st, mx_quantize_segments_kernel<bf16_t><<<dim3((unsigned)blocks), dim3(kQuantThreads), 0, st>>>(
-                                               (const bf16_t*)x, gather, d->k, seg, d->E, K, (char*)codes, (char*)scales));
+  const int64_t row_blocks = mx_max_row_blocks(d);
+  if (row_blocks == 0) return DYNMO_OK;
+  const int parts = parts_of(row_blocks, K);
+  DYNMO_TIMED_LAUNCH(K_MXFP4_QUANTIZE, st, mx_quantize_segments_kernel<bf16_t><<<dim3((unsigned)(row_blocks * parts)), dim3(kQuantThreads), 0, st>>>(
+                                               (const bf16_t*)x, gather, d->k, seg, d->E, K, parts, (char*)codes, (char*)scales));
   return DYNMO_OK;
 }
 
@@ -163,11 +185,13 @@ extern "C" int32_t dynmo_mxfp4_quantize(int32_t n, int32_t rows, int32_t K, int3
   const int32_t rc = check_matrix(n, rows, K, dtype, src, packed, &blocks);
   if (rc || blocks == 0) return rc;
   hipStream_t st = (hipStream_t)stream;
-  const dim3 grid((unsigned)blocks), threads(kQuantThreads);
+  const int64_t row_blocks = (int64_t)n * mx_row_blocks(rows);
+  const int parts = parts_of(row_blocks, K);
+  const dim3 grid((unsigned)(row_blocks * parts)), threads(kQuantThreads);
   if (dtype == DYNMO_BF16) {
-    DYNMO_TIMED_LAUNCH(K_MXFP4_QUANTIZE, st, mx_quantize_kernel<bf16_t><<<grid, threads, 0, st>>>((const bf16_t*)src, (char*)packed, rows, K));
+    DYNMO_TIMED_LAUNCH(K_MXFP4_QUANTIZE, st, mx_quantize_kernel<bf16_t><<<grid, threads, 0, st>>>((const bf16_t*)src, (char*)packed, rows, K, parts));
   } else {
-    DYNMO_TIMED_LAUNCH(K_MXFP4_QUANTIZE, st, mx_quantize_kernel<float><<<grid, threads, 0, st>>>((const float*)src, (char*)packed, rows, K));
+    DYNMO_TIMED_LAUNCH(K_MXFP4_QUANTIZE, st, mx_quantize_kernel<float><<<grid, threads, 0, st>>>((const float*)src, (char*)packed, rows, K, parts));
   }
   return DYNMO_OK;
 }

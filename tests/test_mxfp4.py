@@ -267,7 +267,9 @@ FFN_CASES = [
     (1, 8, 8, 1, 1, [1]), (1, 128, 256, 4, 2, [1, 0, 0, 1]), (3, 136, 72, 2, 2, [6, 0]), (5, 520, 520, 3, 3, [0, 15, 0]),
     (17, 1032, 264, 2, 1, [16, 1]), (40, 256, 640, 4, 2, [33, 0, 30, 17]), (150, 264, 136, 3, 2, [128, 129, 43]),
     (130, 2056, 520, 2, 2, [257, 3]), (70, 512, 1032, 64, 8, [9] * 62 + [0, 2]), (300, 392, 304, 5, 1, [0, 300, 0, 0, 0]),
-    (600, 128, 128, 1, 1, [577])]
+    (600, 128, 128, 1, 1, [577]),
+    # experts that took more rows than there are tokens (a token may name one twice)
+    (16, 264, 136, 4, 4, [40, 0, 3, 20]), (64, 520, 264, 5, 4, [130, 0, 70, 0, 56]), (33, 1544, 1096, 2, 2, [50, 16])]
 
 
 @pytest.mark.gpu
