@@ -4,8 +4,14 @@
 //   s = softmax(z) or sigmoid(z),  v = s + bias;  the top_groups groups with the largest sum of their group_best largest v stay;
 //   of their experts the k with the largest v;  w = s / sum of the chosen s (or s) * scale
 //
-// Which of two experts is ahead is decided on v in 64 bits: of 64 Ki tokens over 256 experts some two have neighbours
-// closer than a 32-bit rounding at the border of the selection, and an index cannot be a little wrong.
+// Which of two experts is ahead is decided on v in 64 bits: of 64 Ki tokens over 256 experts some have neighbours
+// closer than a 32-bit rounding at the border of the selection, and an index cannot be a little wrong.  Done for all of it, 64 bits took
+// ten times the time of the rest, so the selection is made in 32 bits first, with a bound on what their roundings can move; a
+// token with two values in question closer than that (a few in a thousand, and all that have equal ones) is routed again in 64.
+//
+// Bound: at 64 and more experts the vector instructions of the k rounds, below that the launch.  Four (or sixteen) tokens share a
+// wavefront: a maximum over 16 (4) lanes takes four (two) instructions on neighbouring lanes, for all of them at once, and the winner's own
+// lane stores its index and weight, so that nothing else crosses lanes.
 #include "common.h"
 #include "profile.h"
 
@@ -23,204 +29,360 @@ __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
-struct Best {
-  double v;
-  int idx;
-};
-__device__ __forceinline__ Best better(const Best& a, const Best& b) { return a.v > b.v || (a.v == b.v && a.idx < b.idx) ? a : b; }
+// The value that the lane has whose place among LPT neighbours is mirrored in one more bit: after log2(LPT) steps of op(v, neighbour)
+// every lane has the result over all of them.
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int LPT, typename Op>
+__device__ __forceinline__ float over_lanes(float v, Op op) {
+  static_assert(LPT == 4 || LPT == 16, "");
+  v = op(v, moved<0xB1>(v));  // lane ^ 1
+  v = op(v, moved<0x4E>(v));  // lane ^ 2
+  if constexpr (LPT == 16) {
+    v = op(v, moved<0x141>(v));  // 7 - lane of eight
+    v = op(v, moved<0x140>(v));  // 15 - lane of sixteen
+  }
+  return v;
+}
+template <int LPT>
+__device__ __forceinline__ float max_over(float v) {
+  return over_lanes<LPT>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int LPT>
+__device__ __forceinline__ float sum_over(float v) {
+  return over_lanes<LPT>(v, [](float a, float b) { return a + b; });
+}
 
-// A token owns LPT adjacent lanes of a wavefront; lane j of them holds the experts j, j + LPT, ... (VPL of them).
+// A token owns LPT adjacent lanes; lane j of them holds VPL experts, four neighbours each time.
+template <int LPT>
+__device__ __forceinline__ int expert_of(int q, int j) {
+  return q / 4 * (4 * LPT) + j * 4 + q % 4;
+}
+// VEC: E is a multiple of four and the logits are 16-byte aligned
+template <int LPT, int VPL, bool VEC>
+__device__ __forceinline__ void load_logits(const float* __restrict__ row, int j, int E, bool live, float* z) {
+#pragma unroll
+  for (int q = 0; q < VPL; q += 4) {
+    const int e = expert_of<LPT>(q, j);
+    float v[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    if constexpr (VEC) {
+      if (live && e < E) unpack16<float>(*(const u32x4*)(row + e), v);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (live && e + c < E) v[c] = row[e + c];
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) z[q + c] = clean_logit(v[c]);
+  }
+}
+
+// Scores in 32 bits; *top: the largest logit, -inf where there is none (softmax only)
 template <int LPT, int VPL>
+__device__ __forceinline__ void scores32(int score, const float* z, float* s, float* top, float* inv) {
+  if (score == DYNMO_SCORE_SOFTMAX) {
+    float mx = z[0];
+#pragma unroll
+    for (int q = 1; q < VPL; ++q) mx = fmaxf(mx, z[q]);
+    mx = max_over<LPT>(mx);
+    float sum = 0.f;
+#pragma unroll
+    for (int q = 0; q < VPL; ++q) sum += s[q] = z[q] == -INFINITY ? 0.f : __expf(z[q] - mx);
+    sum = sum_over<LPT>(sum);
+    *inv = sum > 0.f ? 1.f / sum : 0.f;
+    *top = mx;
+#pragma unroll
+    for (int q = 0; q < VPL; ++q) s[q] *= *inv;
+  } else {
+#pragma unroll
+    for (int q = 0; q < VPL; ++q) s[q] = sigmoidf_(z[q]);
+  }
+}
+
+// The order values of one token in LDS, by expert; the groups that stay are found from them, and the experts of the others lose their value.
+// *least, *most (32 bits only): the group scores of the last group that stays and of the first that does not.
+template <int LPT, int VPL, typename Real>
+__device__ __forceinline__ void drop_groups(const dynmo_route_rule& rule, int E, int j, Real* order, Real* v, float* least, float* most) {
+  const Real none = -INFINITY;
+#pragma unroll
+  for (int q = 0; q < VPL; ++q)
+    if (expert_of<LPT>(q, j) < E) order[expert_of<LPT>(q, j)] = v[q];
+  wave_lds_order();
+  const int size = E / rule.groups;
+  Real own[VPL];  // the scores of groups j, j + LPT, ..
+#pragma unroll
+  for (int q = 0; q < VPL; ++q) {
+    const int g = q * LPT + j;
+    Real first = none, second = none;
+    for (int i = 0; g < rule.groups && i < size; ++i) {
+      const Real x = order[g * size + i];
+      second = x > first ? first : x > second ? x : second;
+      first = x > first ? x : first;
+    }
+    own[q] = rule.group_best == 2 && second > none ? first + second : first;
+  }
+  wave_lds_order();
+#pragma unroll
+  for (int q = 0; q < VPL; ++q)
+    if (q * LPT + j < rule.groups) order[q * LPT + j] = own[q];
+  wave_lds_order();
+  bool stays[VPL];
+  Real low = INFINITY, high = none;
+#pragma unroll
+  for (int q = 0; q < VPL; ++q) {
+    const int g = q * LPT + j;
+    int before = 0;
+    for (int o = 0; g < rule.groups && o < rule.groups; ++o) {
+      const Real x = order[o];
+      before += x > own[q] || (x == own[q] && o < g);
+    }
+    stays[q] = before < rule.top_groups;
+    if (g < rule.groups) {
+      if (stays[q]) low = own[q] < low ? own[q] : low;
+      else high = own[q] > high ? own[q] : high;
+    }
+  }
+  wave_lds_order();
+#pragma unroll
+  for (int q = 0; q < VPL; ++q)
+    if (q * LPT + j < rule.groups) order[q * LPT + j] = stays[q] ? 1 : 0;
+  wave_lds_order();
+#pragma unroll
+  for (int q = 0; q < VPL; ++q) {
+    const int e = expert_of<LPT>(q, j);
+    if (e < E && order[e / size] == 0) v[q] = none;
+  }
+  wave_lds_order();
+  if constexpr (sizeof(Real) == 4) {
+    *least = -max_over<LPT>(-low);
+    *most = max_over<LPT>(high);
+  }
+}
+
+template <int LPT, int VPL, bool VEC>
 __global__ __launch_bounds__(256) void route_scored_kernel(const float* __restrict__ logits, const float* __restrict__ bias,
                                                            int32_t* __restrict__ expert_idx, float* __restrict__ gate_w, int T, int E,
                                                            int k, const dynmo_route_rule rule) {
   constexpr int kTokens = 64 / LPT;
-  __shared__ double order[4][kTokens][LPT * VPL], scores[4][kTokens][LPT * VPL], group[4][kTokens][LPT * VPL];
+  __shared__ double order[4][kTokens][LPT * VPL];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane % LPT, tok = lane / LPT;
   const long t = ((long)blockIdx.x * 4 + wave) * kTokens + tok;
-  float z[VPL], top = -INFINITY;
-  double s[VPL];
+  const bool live = t < T, softmax = rule.score == DYNMO_SCORE_SOFTMAX;
+  float z[VPL], s[VPL], v[VPL], top = 0.f, inv = 1.f;
+  load_logits<LPT, VPL, VEC>(logits + t * E, j, E, live, z);
+  scores32<LPT, VPL>(rule.score, z, s, &top, &inv);
+  // Scores are monotonous in the logits: without a bias, and without sums of scores, the logits themselves are the order.
+  const bool by_logit = bias == nullptr && (rule.groups == 1 || rule.group_best == 1);
+  float size = 0.f;  // of the largest finite order value
 #pragma unroll
   for (int q = 0; q < VPL; ++q) {
-    const int e = q * LPT + j;
-    z[q] = t < T && e < E ? clean_logit(logits[t * E + e]) : -INFINITY;
-    top = fmaxf(top, z[q]);
-  }
-  if (rule.score == DYNMO_SCORE_SOFTMAX) {
-#pragma unroll
-    for (int m = 1; m < LPT; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
-    double sum = 0.0;
-#pragma unroll
-    for (int q = 0; q < VPL; ++q) sum += s[q] = z[q] == -INFINITY ? 0.0 : exp((double)z[q] - (double)top);
-#pragma unroll
-    for (int m = 1; m < LPT; m <<= 1) sum += __shfl_xor(sum, m, 64);
-#pragma unroll
-    for (int q = 0; q < VPL; ++q) s[q] /= sum > 0.0 ? sum : 1.0;
-  } else {
-#pragma unroll
-    for (int q = 0; q < VPL; ++q) s[q] = 1.0 / (1.0 + exp(-(double)z[q]));
-  }
-  double v[VPL];
-#pragma unroll
-  for (int q = 0; q < VPL; ++q) {
-    const int e = q * LPT + j;
-    v[q] = s[q] + (bias && e < E ? (double)bias[e] : 0.0);
+    const int e = expert_of<LPT>(q, j);
+    v[q] = by_logit ? z[q] : s[q] + (bias && e < E ? bias[e] : 0.f);
     if (!(v[q] > -INFINITY) || z[q] == -INFINITY) v[q] = -INFINITY;
-    order[wave][tok][e] = v[q];
-    scores[wave][tok][e] = s[q];
+    if (fabsf(v[q]) < INFINITY) size = fmaxf(size, fabsf(v[q]));
   }
-  wave_lds_order();
+  // How far apart two order values a >= b have to be for their order to be that of the 64-bit ones.  A score in 32 bits is off by at most
+  // 2^-21 of the largest (an exponential of a rounded difference, x e^-x of which is at most 0.37, a sum of equal signs, a product), twice for
+  // two and four times to be safe; the sum with the bias by 2^-24 of it, twice, and four times.  By logits: the 64-bit scores have
+  // to differ, too: e^z by 2^-40 relative, and the logistic function, whose slope up to z = 16 is at least 2^-24, by 2^-47; where it is flatter
+  // than that, and where both exponentials may vanish, the token is left to the 64 bits.
+  const float upper = by_logit && !softmax ? 16.f : INFINITY, lower = by_logit ? (softmax ? top : 0.f) - 600.f : -INFINITY;
+  auto clear = [&](float a, float b, float larger, float times) {
+    const float apart = !by_logit ? 0x1p-18f * inv + 0x1p-21f * larger : softmax ? 0x1p-40f * (1.f + larger) : 0x1p-23f;
+    return a - b > times * apart && a <= upper && a >= lower;
+  };
+  bool doubtful = false;
   if (rule.groups > 1) {
-    const int size = E / rule.groups;
-    double sum[VPL];
+    size = max_over<LPT>(size);
+    float least, most;
+    drop_groups<LPT, VPL, float>(rule, E, j, (float*)order[wave][tok], v, &least, &most);
+    // sums of two, in which large values may have cancelled each other, or left the range
+    const float larger = by_logit ? fmaxf(fabsf(least), fabsf(most)) : size;
+    doubtful = (most > -INFINITY && !clear(least, most, larger, 2.f)) || (!by_logit && !(size < 1e30f));
+  }
+  int slot[VPL];
 #pragma unroll
-    for (int q = 0; q < VPL; ++q) {
-      const int g = q * LPT + j;
-      double first = -INFINITY, second = -INFINITY;
-      for (int i = 0; g < rule.groups && i < size; ++i) {
-        const double x = order[wave][tok][g * size + i];
-        second = x > first ? first : x > second ? x : second;
-        first = x > first ? x : first;
-      }
-      sum[q] = rule.group_best == 2 && second > -INFINITY ? first + second : first;
-      group[wave][tok][g] = sum[q];
+  for (int q = 0; q < VPL; ++q) slot[q] = -1;
+  float last = INFINITY;
+  int filled = 0;
+  for (int n = 0; n <= k; ++n) {  // one round more: the first that is not chosen
+    float best = v[0];
+#pragma unroll
+    for (int q = 1; q < VPL; ++q) best = fmaxf(best, v[q]);
+    best = max_over<LPT>(best);
+    if (best > -INFINITY) {
+      doubtful |= n > 0 && !clear(last, best, fmaxf(fabsf(last), fabsf(best)), 1.f);
+      filled = n < k ? n + 1 : filled;
     }
-    wave_lds_order();
-    bool stays[VPL];
+    last = best;
+    if (n == k) break;
 #pragma unroll
     for (int q = 0; q < VPL; ++q) {
-      const int g = q * LPT + j;
-      int ahead = 0;
-      for (int o = 0; o < rule.groups; ++o) {
-        const double x = group[wave][tok][o];
-        ahead += x > sum[q] || (x == sum[q] && o < g);
-      }
-      stays[q] = ahead < rule.top_groups;
-    }
-    wave_lds_order();
-#pragma unroll
-    for (int q = 0; q < VPL; ++q) group[wave][tok][q * LPT + j] = stays[q] ? 1.0 : 0.0;
-    wave_lds_order();
-#pragma unroll
-    for (int q = 0; q < VPL; ++q) {
-      const int e = q * LPT + j;
-      if (e < E && group[wave][tok][e / size] == 0.0) v[q] = -INFINITY;
+      const bool taken = v[q] == best && best > -INFINITY;
+      slot[q] = taken ? n : slot[q];
+      v[q] = taken ? -INFINITY : v[q];
     }
   }
-  int idx[VPL];
-  double w[VPL], total = 0.0;
-#pragma unroll
-  for (int q = 0; q < VPL; ++q) idx[q] = -1, w[q] = 0.0;
-  for (int slot = 0; slot < k; ++slot) {
-    Best best = {v[0], j};
-#pragma unroll
-    for (int q = 1; q < VPL; ++q) best = better(best, Best{v[q], q * LPT + j});
-#pragma unroll
-    for (int m = 1; m < LPT; m <<= 1) best = better(best, Best{__shfl_xor(best.v, m, 64), __shfl_xor(best.idx, m, 64)});
-    if (best.v == -INFINITY) best.idx = -1;
-    const double score = best.idx < 0 ? 0.0 : scores[wave][tok][best.idx];
-    total += score;
-#pragma unroll
-    for (int q = 0; q < VPL; ++q) {
-      if (q * LPT + j == slot) {
-        idx[q] = best.idx;
-        w[q] = score;
-      }
-      if (q * LPT + j == best.idx) v[q] = -INFINITY;  // taken
-    }
-  }
-  const double by = rule.renormalize ? (total > 0.0 ? (double)rule.scale / total : 0.0) : (double)rule.scale;
+  float total = 0.f, taken = 0.f;
 #pragma unroll
   for (int q = 0; q < VPL; ++q) {
-    const int slot = q * LPT + j;
-    if (t < T && slot < k) {
-      expert_idx[t * k + slot] = idx[q];
-      gate_w[t * k + slot] = (float)(w[q] * by);
+    total += slot[q] >= 0 ? s[q] : 0.f;
+    taken += slot[q] >= 0 ? 1.f : 0.f;
+  }
+  total = sum_over<LPT>(total);
+  taken = sum_over<LPT>(taken);
+  const float by = rule.renormalize ? (total > 0.f ? rule.scale / total : 0.f) : rule.scale;
+#pragma unroll
+  for (int q = 0; q < VPL; ++q) s[q] *= by;
+  doubtful |= taken != (float)filled;                                          // equal values were taken together
+  doubtful |= rule.renormalize && filled > 0 && !(total > 0x1p-10f);  // small scores, whose exponentials are less exact
+  doubtful &= live;
+  if (__ballot(doubtful)) {  // all lanes of the wavefront go along
+    double s64[VPL], v64[VPL], sum64 = 0.0;
+#pragma unroll
+    for (int q = 0; q < VPL; ++q) {
+      s64[q] = softmax ? (z[q] == -INFINITY ? 0.0 : exp((double)z[q] - (double)top)) : 1.0 / (1.0 + exp(-(double)z[q]));
+      sum64 += s64[q];
     }
+    if (softmax) {
+#pragma unroll
+      for (int m = 1; m < LPT; m <<= 1) sum64 += __shfl_xor(sum64, m, 64);
+    }
+#pragma unroll
+    for (int q = 0; q < VPL; ++q) {
+      const int e = expert_of<LPT>(q, j);
+      if (softmax) s64[q] /= sum64 > 0.0 ? sum64 : 1.0;
+      v64[q] = s64[q] + (bias && e < E ? (double)bias[e] : 0.0);
+      if (!(v64[q] > -INFINITY) || z[q] == -INFINITY) v64[q] = -INFINITY;
+    }
+    if (rule.groups > 1) drop_groups<LPT, VPL, double>(rule, E, j, order[wave][tok], v64, nullptr, nullptr);
+    int slot64[VPL], filled64 = 0;
+#pragma unroll
+    for (int q = 0; q < VPL; ++q) slot64[q] = -1;
+    for (int n = 0; n < k; ++n) {
+      double best = v64[0];
+      int at = expert_of<LPT>(0, j);
+#pragma unroll
+      for (int q = 1; q < VPL; ++q)  // experts ascend with q
+        if (v64[q] > best) best = v64[q], at = expert_of<LPT>(q, j);
+#pragma unroll
+      for (int m = 1; m < LPT; m <<= 1) {
+        const double o = __shfl_xor(best, m, 64);
+        const int o_at = __shfl_xor(at, m, 64);
+        if (o > best || (o == best && o_at < at)) best = o, at = o_at;
+      }
+      if (!(best > -INFINITY)) break;
+      filled64 = n + 1;
+#pragma unroll
+      for (int q = 0; q < VPL; ++q) {
+        const bool mine = expert_of<LPT>(q, j) == at;
+        slot64[q] = mine ? n : slot64[q];
+        v64[q] = mine ? -INFINITY : v64[q];
+      }
+    }
+    double total64 = 0.0;
+#pragma unroll
+    for (int q = 0; q < VPL; ++q) total64 += slot64[q] >= 0 ? s64[q] : 0.0;
+#pragma unroll
+    for (int m = 1; m < LPT; m <<= 1) total64 += __shfl_xor(total64, m, 64);
+    const double over64 = rule.renormalize && total64 > 0.0 ? total64 : 1.0;  // divided by: it may be subnormal (or zero, as all its terms are)
+    if (sum_over<LPT>(doubtful ? 1.f : 0.f) > 0.f) {
+      filled = filled64;
+#pragma unroll
+      for (int q = 0; q < VPL; ++q) {
+        slot[q] = slot64[q];
+        s[q] = (float)(s64[q] / over64 * rule.scale);
+      }
+    }
+  }
+  if (!live) return;
+#pragma unroll
+  for (int q = 0; q < VPL; ++q)
+    if (slot[q] >= 0) {
+      expert_idx[t * k + slot[q]] = expert_of<LPT>(q, j);
+      gate_w[t * k + slot[q]] = s[q];
+    }
+  for (int n = filled + j; n < k; n += LPT) {  // no expert is left for these
+    expert_idx[t * k + n] = -1;
+    gate_w[t * k + n] = 0.f;
   }
 }
 
 // ds_j = (g_j - sum_i g_i s_i / S) / S with S the sum of the chosen scores (or g_j), g = dgate * scale; then through the scores:
 // sigmoid ds s (1 - s) at the chosen experts, softmax p_e ([e chosen] ds_e - sum_j ds_j p_j) everywhere.
-template <int LPT, int VPL>
+// Bound by memory: the sigmoid reads the chosen logits only.  The slots' gradients meet their experts in an LDS row per token, slot after
+// slot, so that an expert in several slots gets their sum in a fixed order.
+template <int LPT, int VPL, bool VEC>
 __global__ __launch_bounds__(256) void route_scored_bwd_kernel(const float* __restrict__ dgate, const float* __restrict__ logits,
                                                                const int32_t* __restrict__ expert_idx, float* __restrict__ dlogits,
                                                                int T, int E, int k, const dynmo_route_rule rule) {
   constexpr int kTokens = 64 / LPT;
-  __shared__ float scores[4][kTokens][LPT * VPL], grads[4][kTokens][LPT * VPL];
-  __shared__ int chosen[4][kTokens][LPT * VPL];
+  __shared__ __attribute__((aligned(16))) float grads[4][kTokens][LPT * VPL];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane % LPT, tok = lane / LPT;
   const long t = ((long)blockIdx.x * 4 + wave) * kTokens + tok;
-  float z[VPL], s[VPL], top = -INFINITY;
-#pragma unroll
-  for (int q = 0; q < VPL; ++q) {
-    const int e = q * LPT + j;
-    z[q] = t < T && e < E ? clean_logit(logits[t * E + e]) : -INFINITY;
-    top = fmaxf(top, z[q]);
-  }
-  if (rule.score == DYNMO_SCORE_SOFTMAX) {
-#pragma unroll
-    for (int m = 1; m < LPT; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
-    float sum = 0.f;
-#pragma unroll
-    for (int q = 0; q < VPL; ++q) sum += s[q] = z[q] == -INFINITY ? 0.f : __expf(z[q] - top);
-#pragma unroll
-    for (int m = 1; m < LPT; m <<= 1) sum += __shfl_xor(sum, m, 64);
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
-#pragma unroll
-    for (int q = 0; q < VPL; ++q) s[q] *= inv;
-  } else {
-#pragma unroll
-    for (int q = 0; q < VPL; ++q) s[q] = sigmoidf_(z[q]);
+  const bool live = t < T, softmax = rule.score == DYNMO_SCORE_SOFTMAX;
+  float* const row = grads[wave][tok];
+  const float* const lg = logits + t * E;
+  float z[VPL], s[VPL], top = 0.f, inv = 1.f;
+  if (softmax) {
+    load_logits<LPT, VPL, VEC>(lg, j, E, live, z);
+    scores32<LPT, VPL>(rule.score, z, s, &top, &inv);
   }
 #pragma unroll
-  for (int q = 0; q < VPL; ++q) scores[wave][tok][q * LPT + j] = s[q];
+  for (int q = 0; q < VPL; q += 4) *(u32x4*)(row + expert_of<LPT>(q, j)) = u32x4{0u, 0u, 0u, 0u};
   wave_lds_order();
-  float g[VPL], w[VPL], total = 0.f, inner = 0.f;
-  int idx[VPL];
-#pragma unroll
-  for (int q = 0; q < VPL; ++q) {
-    const int slot = q * LPT + j;
-    const bool used = t < T && slot < k;
-    idx[q] = used ? expert_idx[t * k + slot] : -1;
-    if (idx[q] < 0 || idx[q] >= E) idx[q] = -1;
-    g[q] = idx[q] >= 0 ? dgate[t * k + slot] * rule.scale : 0.f;
-    w[q] = idx[q] >= 0 ? scores[wave][tok][idx[q]] : 0.f;
-    total += w[q];
-    inner += g[q] * w[q];
+  // slot `n` of the token: its expert (-1: none), that expert's score, the slope of the logistic function there, and the gradient
+  auto slot = [&](int n, float* score, float* slope, float* g) {
+    *score = *slope = *g = 0.f;
+    if (!live || n >= k) return -1;
+    const int e = expert_idx[t * k + n];
+    if (e < 0 || e >= E) return -1;
+    const float x = clean_logit(lg[e]);
+    *score = softmax ? (x == -INFINITY ? 0.f : __expf(x - top) * inv) : sigmoidf_(x);
+    *slope = softmax ? 1.f : *score * sigmoidf_(-x);
+    *g = dgate[t * k + n] * rule.scale;
+    return e;
+  };
+  float total = 0.f, inner = 0.f, score, slope, g;
+  int e = -1;
+  for (int n = j; n < k; n += LPT) {
+    e = slot(n, &score, &slope, &g);
+    total += score;
+    inner += g * score;
   }
-#pragma unroll
-  for (int m = 1; m < LPT; m <<= 1) {
-    total += __shfl_xor(total, m, 64);
-    inner += __shfl_xor(inner, m, 64);
-  }
-  if (rule.renormalize) {
-    const float inv = total > 0.f ? 1.f / total : 0.f;
-#pragma unroll
-    for (int q = 0; q < VPL; ++q) g[q] = idx[q] >= 0 ? (g[q] - inner * inv) * inv : 0.f;
-    inner = 0.f;  // sum_j ds_j s_j
-  }
-#pragma unroll
-  for (int q = 0; q < VPL; ++q) {
-    chosen[wave][tok][q * LPT + j] = idx[q];
-    grads[wave][tok][q * LPT + j] = g[q];
+  total = sum_over<LPT>(total);
+  inner = sum_over<LPT>(inner);
+  const float by = total > 0.f ? 1.f / total : 0.f;
+  for (int base = 0; base < k; base += LPT) {
+    if (k > LPT || j >= k) e = slot(base + j, &score, &slope, &g);  // else it is still there
+    const float ds = (rule.renormalize ? (g - inner * by) * by : g) * slope;
+    for (int i = 0; i < LPT && base + i < k; ++i) {
+      if (j == i && e >= 0) __hip_atomic_fetch_add(row + e, ds, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+      wave_lds_order();
+    }
   }
   wave_lds_order();
-  float ds[VPL];
+  if (rule.renormalize) inner = 0.f;  // sum_j ds_j s_j
+  if (!live) return;
+  float* const out = dlogits + t * E;
 #pragma unroll
-  for (int q = 0; q < VPL; ++q) ds[q] = 0.f;
-  for (int slot = 0; slot < k; ++slot) {
-    const int e = chosen[wave][tok][slot];
-    const float d = grads[wave][tok][slot];
+  for (int q = 0; q < VPL; q += 4) {
+    const int at = expert_of<LPT>(q, j);
+    float d[4];
+    unpack16<float>(*(const u32x4*)(row + at), d);
+    if (softmax) {
 #pragma unroll
-    for (int q = 0; q < VPL; ++q)
-      if (e == q * LPT + j) ds[q] += d;
-  }
+      for (int c = 0; c < 4; ++c) d[c] = s[q + c] * (d[c] - inner);
+    }
+    if constexpr (VEC) {
+      if (at < E) *(u32x4*)(out + at) = pack16<float>(d);
+    } else {
 #pragma unroll
-  for (int q = 0; q < VPL; ++q) {
-    const int e = q * LPT + j;
-    if (t < T && e < E)
-      dlogits[t * E + e] = rule.score == DYNMO_SCORE_SOFTMAX ? s[q] * (ds[q] - inner) : ds[q] == 0.f ? 0.f : ds[q] * s[q] * sigmoidf_(-z[q]);
+      for (int c = 0; c < 4; ++c)
+        if (at + c < E) out[at + c] = d[c];
+    }
   }
 }
 
@@ -235,20 +397,18 @@ static int32_t check_route(const dynmo_desc* d, const dynmo_route_rule* r) {
   return DYNMO_OK;
 }
 
-// f(lanes per token, experts per lane) for this number of experts
+// f(lanes per token, experts per lane, whether rows can be read 16 bytes at a time).  Fewer lanes per token for few experts: 16 tokens per
+// wavefront instead of 4.
 template <typename F>
-static int32_t by_experts(int E, F&& f) {
+static int32_t by_experts(int E, bool aligned, F&& f) {
   using std::integral_constant;
-  const integral_constant<int, 1> one;
-  if (E <= 1) return f(one, one);
-  if (E <= 2) return f(integral_constant<int, 2>{}, one);
-  if (E <= 4) return f(integral_constant<int, 4>{}, one);
-  if (E <= 8) return f(integral_constant<int, 8>{}, one);
-  if (E <= 16) return f(integral_constant<int, 16>{}, one);
-  if (E <= 32) return f(integral_constant<int, 32>{}, one);
-  if (E <= 64) return f(integral_constant<int, 64>{}, one);
-  if (E <= 128) return f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-  return f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  auto with = [&](auto lpt, auto vpl) -> int32_t {
+    return E % 4 == 0 && aligned ? f(lpt, vpl, std::true_type{}) : f(lpt, vpl, std::false_type{});
+  };
+  if (E <= 16) return with(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+  if (E <= 64) return with(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+  if (E <= 128) return with(integral_constant<int, 16>{}, integral_constant<int, 8>{});
+  return with(integral_constant<int, 16>{}, integral_constant<int, 16>{});
 }
 
 static dim3 blocks_of(int T, int tokens_per_wave) { return dim3((unsigned)((T + 4L * tokens_per_wave - 1) / (4L * tokens_per_wave))); }
@@ -263,10 +423,10 @@ extern "C" int32_t dynmo_route_scored(const dynmo_desc* d, const dynmo_route_rul
   if (rc) return rc;
   if (!logits || !expert_idx || !gate_w) return DYNMO_EINVAL;
   if (d->T == 0) return DYNMO_OK;
-  return by_experts(d->E, [&](auto lpt, auto vpl) -> int32_t {
+  return by_experts(d->E, !misaligned16(logits), [&](auto lpt, auto vpl, auto vec) -> int32_t {
     constexpr int LPT = decltype(lpt)::value, VPL = decltype(vpl)::value;
     hipStream_t st = (hipStream_t)stream;
-    DYNMO_TIMED_LAUNCH(K_ROUTE_TOPK, st, route_scored_kernel<LPT, VPL><<<blocks_of(d->T, 64 / LPT), dim3(256), 0, st>>>(
+    DYNMO_TIMED_LAUNCH(K_ROUTE_TOPK, st, route_scored_kernel<LPT, VPL, decltype(vec)::value><<<blocks_of(d->T, 64 / LPT), dim3(256), 0, st>>>(
                                              logits, bias, expert_idx, gate_w, d->T, d->E, d->k, *rule));
     return DYNMO_OK;
   });
@@ -278,11 +438,12 @@ extern "C" int32_t dynmo_route_scored_bwd(const dynmo_desc* d, const dynmo_route
   if (rc) return rc;
   if (!dgate || !logits || !expert_idx || !dlogits) return DYNMO_EINVAL;
   if (d->T == 0) return DYNMO_OK;
-  return by_experts(d->E, [&](auto lpt, auto vpl) -> int32_t {
+  return by_experts(d->E, !misaligned16(logits, dlogits), [&](auto lpt, auto vpl, auto vec) -> int32_t {
     constexpr int LPT = decltype(lpt)::value, VPL = decltype(vpl)::value;
     hipStream_t st = (hipStream_t)stream;
-    DYNMO_TIMED_LAUNCH(K_ROUTE_TOPK_BWD, st, route_scored_bwd_kernel<LPT, VPL><<<blocks_of(d->T, 64 / LPT), dim3(256), 0, st>>>(
-                                                 dgate, logits, expert_idx, dlogits, d->T, d->E, d->k, *rule));
+    DYNMO_TIMED_LAUNCH(K_ROUTE_TOPK_BWD, st,
+                       route_scored_bwd_kernel<LPT, VPL, decltype(vec)::value><<<blocks_of(d->T, 64 / LPT), dim3(256), 0, st>>>(
+                           dgate, logits, expert_idx, dlogits, d->T, d->E, d->k, *rule));
     return DYNMO_OK;
   });
 }

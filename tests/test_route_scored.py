@@ -228,6 +228,29 @@ def test_bias_of_infinities_and_nan():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,groups,top", [(12, 1, 1), (48, 6, 2), (160, 5, 3)])
+def test_scores_that_vanish_or_saturate(score, E, groups, top):
+    """The chosen experts far below the largest logit (kept off it by the bias), logits whose scores are one or zero in 64 bits, and biases of
+    the type's lowest value, alone and in pairs that overflow."""
+    rng = np.random.default_rng(E)
+    T = 60
+    lg = rng.standard_normal((T, E)).astype(np.float32)
+    lg[:20, 1] += 60.0
+    lg[20:30] += 45.0
+    lg[30:40] *= 300.0
+    lg[40:50] -= 800.0
+    low = np.finfo(np.float32).min
+    for bias in (None, np.where(np.arange(E) == 1, -np.inf, 0), np.where(np.arange(E) % 3 == 1, low, 0), np.full(E, low),
+                 np.where(np.arange(E) % 2 == 1, 3e38, -3e38)):
+        bias = None if bias is None else (bias + 0.01 * rng.standard_normal(E)).astype(np.float32)
+        for best in (1, 2):
+            rule = dict(score=score, groups=groups, top_groups=top, group_best=best, renormalize=True, scale=1.0)
+            check_route(lg, bias, 3, rule)
+            check_route(lg, bias, 3, dict(rule, renormalize=False))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 def test_many_tokens_close_to_the_border(score):
     """A large batch, where some tokens' k-th and next order value differ by less than an fp32 rounding: the indices are still those of the
     64-bit order.  The reference order is taken by torch in 64 bits."""
