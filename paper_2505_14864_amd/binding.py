@@ -352,14 +352,18 @@ def dynmo_mxfp4_bytes(rows, K):
     return lib().dynmo_mxfp4_bytes(int(rows), int(K))
 
 
+_MXFP4_TYPES = {torch.float32: DYNMO_F32, torch.bfloat16: DYNMO_BF16}
+
+
 def _mxfp4_sizes(values, packed):
     """n, rows, K and the type of a tensor [n, rows, K] or [rows, K] whose packed form is `packed`."""
-    code = {torch.float32: DYNMO_F32, torch.bfloat16: DYNMO_BF16}.get(values.dtype)
-    if code is None or values.dim() not in (2, 3) or packed.dtype != torch.uint8:
+    code, shape = _MXFP4_TYPES.get(values.dtype), values.shape
+    if code is None or len(shape) not in (2, 3) or packed.dtype != torch.uint8:
         raise ValueError("expected float32 or bfloat16 [n, rows, K] or [rows, K], packed as uint8")
-    n, (rows, K) = values.shape[0] if values.dim() == 3 else 1, values.shape[-2:]
-    if packed.numel() != n * dynmo_mxfp4_bytes(rows, K):
-        raise ValueError("packed holds %d bytes, these matrices take %d" % (packed.numel(), n * dynmo_mxfp4_bytes(rows, K)))
+    n, rows, K = shape if len(shape) == 3 else (1, *shape)
+    size = n * ((rows + 15) // 16) * ((K + 127) // 128 * 1024 + (K + 511) // 512 * 256)  # dynmo_mxfp4_bytes() without the call
+    if packed.numel() != size:
+        raise ValueError("packed holds %d bytes, these matrices take %d" % (packed.numel(), size))
     return n, rows, K, code
 
 

@@ -9,9 +9,12 @@
 // ten times the time of the rest, so the selection is made in 32 bits first, with a bound on what their roundings can move; a
 // token with two values in question closer than that (a few in a thousand, and all that have equal ones) is routed again in 64.
 //
-// Bound: at 64 and more experts the vector instructions of the k rounds, below that the launch.  Four (or sixteen) tokens share a
-// wavefront: a maximum over 16 (4) lanes takes four (two) instructions on neighbouring lanes, for all of them at once, and the winner's own
-// lane stores its index and weight, so that nothing else crosses lanes.
+// Bound: the vector instructions of the k rounds, with few tokens the launch and their latency.  A lane holds four neighbouring experts, a token
+// as many lanes as it needs, 4, 16 or 64, so that up to 16 tokens share a wavefront; a maximum over a token's lanes takes two, four or
+// eight vector instructions for all of them at once, and the winner's own lane stores its index and weight: nothing else crosses lanes.
+//
+// Measured: 65536 tokens x 64 experts, k = 8, with a bias 20 us (all of it in 64 bits, a token per wavefront: 101), 4096 x 256 in eight groups 14
+// (18; of these 14 the doubtful tokens are 4), 3001 x 60 in five groups 5 (9), one token 2.3; backward 65536 x 256 22 us, 3 TB/s of gradients written.
 #include "common.h"
 #include "profile.h"
 
@@ -37,12 +40,18 @@ __device__ __forceinline__ float moved(float v) {
 }
 template <int LPT, typename Op>
 __device__ __forceinline__ float over_lanes(float v, Op op) {
-  static_assert(LPT == 4 || LPT == 16, "");
+  static_assert(LPT == 4 || LPT == 16 || LPT == 64, "");
   v = op(v, moved<0xB1>(v));  // lane ^ 1
   v = op(v, moved<0x4E>(v));  // lane ^ 2
-  if constexpr (LPT == 16) {
+  if constexpr (LPT >= 16) {
     v = op(v, moved<0x141>(v));  // 7 - lane of eight
     v = op(v, moved<0x140>(v));  // 15 - lane of sixteen
+  }
+  if constexpr (LPT == 64) {  // a swap of two copies leaves the two halves of each pair of rows, and of the wavefront, everywhere
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
   }
   return v;
 }
@@ -53,6 +62,38 @@ __device__ __forceinline__ float max_over(float v) {
 template <int LPT>
 __device__ __forceinline__ float sum_over(float v) {
   return over_lanes<LPT>(v, [](float a, float b) { return a + b; });
+}
+
+// The first in the order of two experts, and of all the token's
+struct Ranked {
+  double v;
+  int e;
+};
+__device__ __forceinline__ Ranked ahead_of(Ranked a, Ranked b) { return b.v > a.v || (b.v == a.v && b.e < a.e) ? b : a; }
+template <int CTRL>
+__device__ __forceinline__ Ranked moved(Ranked r) {
+  const long long w = __double_as_longlong(r.v);
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)w, CTRL, 0xf, 0xf, true), hi = __builtin_amdgcn_update_dpp(0, (int)(w >> 32), CTRL, 0xf, 0xf, true);
+  return {__longlong_as_double((long long)hi << 32 | (uint32_t)lo), __builtin_amdgcn_update_dpp(0, r.e, CTRL, 0xf, 0xf, true)};
+}
+template <int LPT>
+__device__ __forceinline__ Ranked first_over(Ranked r) {
+  r = ahead_of(r, moved<0xB1>(r));
+  r = ahead_of(r, moved<0x4E>(r));
+  if constexpr (LPT >= 16) {
+    r = ahead_of(r, moved<0x141>(r));
+    r = ahead_of(r, moved<0x140>(r));
+  }
+  if constexpr (LPT == 64) {
+    auto both = [&](auto swap) {
+      const long long w = __double_as_longlong(r.v);
+      const auto lo = swap((uint32_t)w), hi = swap((uint32_t)(w >> 32)), e = swap((uint32_t)r.e);
+      r = ahead_of({__longlong_as_double((long long)hi[0] << 32 | lo[0]), (int)e[0]}, {__longlong_as_double((long long)hi[1] << 32 | lo[1]), (int)e[1]});
+    };
+    both([](uint32_t x) { return __builtin_amdgcn_permlane16_swap(x, x, false, false); });
+    both([](uint32_t x) { return __builtin_amdgcn_permlane32_swap(x, x, false, false); });
+  }
+  return r;
 }
 
 // A token owns LPT adjacent lanes; lane j of them holds VPL experts, four neighbours each time.
@@ -101,58 +142,84 @@ __device__ __forceinline__ void scores32(int score, const float* z, float* s, fl
   }
 }
 
-// The order values of one token in LDS, by expert; the groups that stay are found from them, and the experts of the others lose their value.
+// The experts of the groups that do not stay lose their order value.  `order`: an LDS row of 4 LPT values for this token.
 // *least, *most (32 bits only): the group scores of the last group that stays and of the first that does not.
-template <int LPT, int VPL, typename Real>
+template <int LPT, typename Real>
 __device__ __forceinline__ void drop_groups(const dynmo_route_rule& rule, int E, int j, Real* order, Real* v, float* least, float* most) {
   const Real none = -INFINITY;
-#pragma unroll
-  for (int q = 0; q < VPL; ++q)
-    if (expert_of<LPT>(q, j) < E) order[expert_of<LPT>(q, j)] = v[q];
-  wave_lds_order();
-  const int size = E / rule.groups;
-  Real own[VPL];  // the scores of groups j, j + LPT, ..
-#pragma unroll
-  for (int q = 0; q < VPL; ++q) {
-    const int g = q * LPT + j;
-    Real first = none, second = none;
-    for (int i = 0; g < rule.groups && i < size; ++i) {
-      const Real x = order[g * size + i];
-      second = x > first ? first : x > second ? x : second;
-      first = x > first ? x : first;
-    }
-    own[q] = rule.group_best == 2 && second > none ? first + second : first;
-  }
-  wave_lds_order();
-#pragma unroll
-  for (int q = 0; q < VPL; ++q)
-    if (q * LPT + j < rule.groups) order[q * LPT + j] = own[q];
-  wave_lds_order();
-  bool stays[VPL];
+  const int size = E / rule.groups, lane = threadIdx.x & 63;
+  auto add = [&](Real x, Real* first, Real* second) {
+    *second = x > *first ? *first : x > *second ? x : *second;
+    *first = x > *first ? x : *first;
+  };
+  auto score = [&](Real first, Real second) { return rule.group_best == 2 && second > none ? first + second : first; };
   Real low = INFINITY, high = none;
-#pragma unroll
-  for (int q = 0; q < VPL; ++q) {
-    const int g = q * LPT + j;
+  auto count = [&](Real own, int g) {  // whether group g stays
     int before = 0;
-    for (int o = 0; g < rule.groups && o < rule.groups; ++o) {
+#pragma unroll 4
+    for (int o = 0; o < rule.groups; ++o) {
       const Real x = order[o];
-      before += x > own[q] || (x == own[q] && o < g);
+      before += x > own || (x == own && o < g);
     }
-    stays[q] = before < rule.top_groups;
-    if (g < rule.groups) {
-      if (stays[q]) low = own[q] < low ? own[q] : low;
-      else high = own[q] > high ? own[q] : high;
+    const bool stays = before < rule.top_groups;
+    if (stays) low = own < low ? own : low;
+    else high = own > high ? own : high;
+    return stays;
+  };
+  if (size % 4 == 0) {  // a lane's experts are of one group, and no group has more than one lane to look after it
+    Real first = none, second = none;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) add(v[q], &first, &second);
+    order[2 * j] = first;
+    order[2 * j + 1] = second;
+    wave_lds_order();
+    first = second = none;
+    if (j < rule.groups) {
+#pragma unroll 4
+      for (int i = 0; i < size / 4; ++i) {
+        add(order[2 * (j * (size / 4) + i)], &first, &second);
+        add(order[2 * (j * (size / 4) + i) + 1], &first, &second);
+      }
     }
-  }
-  wave_lds_order();
+    wave_lds_order();
+    const Real own = score(first, second);
+    order[j] = own;
+    wave_lds_order();
+    const bool stays = j < rule.groups && count(own, j);
+    const unsigned long long kept = __ballot(stays) >> (lane - j);
+    if (4 * j < E && !(kept >> (4 * j / size) & 1)) {
 #pragma unroll
-  for (int q = 0; q < VPL; ++q)
-    if (q * LPT + j < rule.groups) order[q * LPT + j] = stays[q] ? 1 : 0;
-  wave_lds_order();
+      for (int q = 0; q < 4; ++q) v[q] = none;
+    }
+  } else {
 #pragma unroll
-  for (int q = 0; q < VPL; ++q) {
-    const int e = expert_of<LPT>(q, j);
-    if (e < E && order[e / size] == 0) v[q] = none;
+    for (int q = 0; q < 4; ++q) order[4 * j + q] = v[q];
+    wave_lds_order();
+    Real own[4];  // the scores of groups j, j + LPT, ..
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int g = q * LPT + j;
+      Real first = none, second = none;
+      if (g < rule.groups) {
+#pragma unroll 4
+        for (int i = 0; i < size; ++i) add(order[g * size + i], &first, &second);
+      }
+      own[q] = score(first, second);
+    }
+    wave_lds_order();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) order[q * LPT + j] = own[q];
+    wave_lds_order();
+    bool stays[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) stays[q] = q * LPT + j < rule.groups && count(own[q], q * LPT + j);
+    wave_lds_order();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) order[q * LPT + j] = stays[q] ? 1 : 0;
+    wave_lds_order();
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (4 * j + q < E && order[(4 * j + q) / size] == 0) v[q] = none;
   }
   wave_lds_order();
   if constexpr (sizeof(Real) == 4) {
@@ -161,11 +228,11 @@ __device__ __forceinline__ void drop_groups(const dynmo_route_rule& rule, int E,
   }
 }
 
-template <int LPT, int VPL, bool VEC>
+template <int LPT, bool VEC>
 __global__ __launch_bounds__(256) void route_scored_kernel(const float* __restrict__ logits, const float* __restrict__ bias,
                                                            int32_t* __restrict__ expert_idx, float* __restrict__ gate_w, int T, int E,
                                                            int k, const dynmo_route_rule rule) {
-  constexpr int kTokens = 64 / LPT;
+  constexpr int kTokens = 64 / LPT, VPL = 4;
   __shared__ double order[4][kTokens][LPT * VPL];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane % LPT, tok = lane / LPT;
   const long t = ((long)blockIdx.x * 4 + wave) * kTokens + tok;
@@ -189,34 +256,37 @@ __global__ __launch_bounds__(256) void route_scored_kernel(const float* __restri
   // to differ, too: e^z by 2^-40 relative, and the logistic function, whose slope up to z = 16 is at least 2^-24, by 2^-47; where it is flatter
   // than that, and where both exponentials may vanish, the token is left to the 64 bits.
   const float upper = by_logit && !softmax ? 16.f : INFINITY, lower = by_logit ? (softmax ? top : 0.f) - 600.f : -INFINITY;
-  auto clear = [&](float a, float b, float larger, float times) {
-    const float apart = !by_logit ? 0x1p-18f * inv + 0x1p-21f * larger : softmax ? 0x1p-40f * (1.f + larger) : 0x1p-23f;
-    return a - b > times * apart && a <= upper && a >= lower;
-  };
-  bool doubtful = false;
+  auto apart = [&](float larger) { return !by_logit ? 0x1p-18f * inv + 0x1p-21f * larger : softmax ? 0x1p-40f * (1.f + larger) : 0x1p-23f; };
+  bool doubtful = false, doubtful_groups = false;
   if (rule.groups > 1) {
     size = max_over<LPT>(size);
     float least, most;
-    drop_groups<LPT, VPL, float>(rule, E, j, (float*)order[wave][tok], v, &least, &most);
+    drop_groups<LPT, float>(rule, E, j, (float*)order[wave][tok], v, &least, &most);
     // sums of two, in which large values may have cancelled each other, or left the range
     const float larger = by_logit ? fmaxf(fabsf(least), fabsf(most)) : size;
-    doubtful = (most > -INFINITY && !clear(least, most, larger, 2.f)) || (!by_logit && !(size < 1e30f));
+    doubtful_groups = (most > -INFINITY && !(least - most > 2.f * apart(larger) && least <= upper && least >= lower)) || (!by_logit && !(size < 1e30f));
   }
   int slot[VPL];
+  bool can[VPL];
 #pragma unroll
-  for (int q = 0; q < VPL; ++q) slot[q] = -1;
-  float last = INFINITY;
+  for (int q = 0; q < VPL; ++q) {
+    slot[q] = -1;
+    can[q] = v[q] > -INFINITY;
+  }
+  float last = NAN, largest = -INFINITY, gap = INFINITY;
   int filled = 0;
   for (int n = 0; n <= k; ++n) {  // one round more: the first that is not chosen
     float best = v[0];
 #pragma unroll
     for (int q = 1; q < VPL; ++q) best = fmaxf(best, v[q]);
     best = max_over<LPT>(best);
+    if (n == 0) largest = best;
     if (best > -INFINITY) {
-      doubtful |= n > 0 && !clear(last, best, fmaxf(fabsf(last), fabsf(best)), 1.f);
+      gap = fminf(gap, last - best);  // equal infinities leave no gap, but are taken together
+      doubtful = last < lower;
+      last = best;
       filled = n < k ? n + 1 : filled;
     }
-    last = best;
     if (n == k) break;
 #pragma unroll
     for (int q = 0; q < VPL; ++q) {
@@ -225,6 +295,7 @@ __global__ __launch_bounds__(256) void route_scored_kernel(const float* __restri
       v[q] = taken ? -INFINITY : v[q];
     }
   }
+  doubtful |= filled > 0 && (!(gap > apart(fmaxf(fabsf(largest), fabsf(last)))) || largest > upper);
   float total = 0.f, taken = 0.f;
 #pragma unroll
   for (int q = 0; q < VPL; ++q) {
@@ -238,7 +309,8 @@ __global__ __launch_bounds__(256) void route_scored_kernel(const float* __restri
   for (int q = 0; q < VPL; ++q) s[q] *= by;
   doubtful |= taken != (float)filled;                                          // equal values were taken together
   doubtful |= rule.renormalize && filled > 0 && !(total > 0x1p-10f);  // small scores, whose exponentials are less exact
-  doubtful &= live;
+  doubtful_groups &= live;
+  doubtful = (doubtful || doubtful_groups) && live;
   if (__ballot(doubtful)) {  // all lanes of the wavefront go along
     double s64[VPL], v64[VPL], sum64 = 0.0;
 #pragma unroll
@@ -257,27 +329,24 @@ __global__ __launch_bounds__(256) void route_scored_kernel(const float* __restri
       v64[q] = s64[q] + (bias && e < E ? (double)bias[e] : 0.0);
       if (!(v64[q] > -INFINITY) || z[q] == -INFINITY) v64[q] = -INFINITY;
     }
-    if (rule.groups > 1) drop_groups<LPT, VPL, double>(rule, E, j, order[wave][tok], v64, nullptr, nullptr);
+    if (__ballot(doubtful_groups)) {
+      drop_groups<LPT, double>(rule, E, j, order[wave][tok], v64, nullptr, nullptr);
+    } else {
+#pragma unroll
+      for (int q = 0; q < VPL; ++q) v64[q] = can[q] ? v64[q] : -INFINITY;
+    }
     int slot64[VPL], filled64 = 0;
 #pragma unroll
     for (int q = 0; q < VPL; ++q) slot64[q] = -1;
     for (int n = 0; n < k; ++n) {
-      double best = v64[0];
-      int at = expert_of<LPT>(0, j);
+      Ranked best = {v64[0], expert_of<LPT>(0, j)};
 #pragma unroll
-      for (int q = 1; q < VPL; ++q)  // experts ascend with q
-        if (v64[q] > best) best = v64[q], at = expert_of<LPT>(q, j);
-#pragma unroll
-      for (int m = 1; m < LPT; m <<= 1) {
-        const double o = __shfl_xor(best, m, 64);
-        const int o_at = __shfl_xor(at, m, 64);
-        if (o > best || (o == best && o_at < at)) best = o, at = o_at;
-      }
-      if (!(best > -INFINITY)) break;
-      filled64 = n + 1;
+      for (int q = 1; q < VPL; ++q) best = ahead_of(best, {v64[q], expert_of<LPT>(q, j)});
+      best = first_over<LPT>(best);
+      if (best.v > -INFINITY) filled64 = n + 1;  // lanes of other tokens take part in what follows
 #pragma unroll
       for (int q = 0; q < VPL; ++q) {
-        const bool mine = expert_of<LPT>(q, j) == at;
+        const bool mine = expert_of<LPT>(q, j) == best.e && best.v > -INFINITY;
         slot64[q] = mine ? n : slot64[q];
         v64[q] = mine ? -INFINITY : v64[q];
       }
@@ -397,9 +466,9 @@ static int32_t check_route(const dynmo_desc* d, const dynmo_route_rule* r) {
   return DYNMO_OK;
 }
 
-// f(lanes per token, experts per lane, whether rows can be read 16 bytes at a time).  Fewer lanes per token for few experts: 16 tokens per
-// wavefront instead of 4.
-template <typename F>
+// f(lanes per token, experts per lane, whether rows can be read 16 bytes at a time).  The backward pass has nothing to search for and takes 16
+// lanes per token for more than 64 experts, too.
+template <bool BACKWARD, typename F>
 static int32_t by_experts(int E, bool aligned, F&& f) {
   using std::integral_constant;
   auto with = [&](auto lpt, auto vpl) -> int32_t {
@@ -407,8 +476,9 @@ static int32_t by_experts(int E, bool aligned, F&& f) {
   };
   if (E <= 16) return with(integral_constant<int, 4>{}, integral_constant<int, 4>{});
   if (E <= 64) return with(integral_constant<int, 16>{}, integral_constant<int, 4>{});
-  if (E <= 128) return with(integral_constant<int, 16>{}, integral_constant<int, 8>{});
-  return with(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+  if constexpr (!BACKWARD) return with(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  else if (E <= 128) return with(integral_constant<int, 16>{}, integral_constant<int, 8>{});
+  else return with(integral_constant<int, 16>{}, integral_constant<int, 16>{});
 }
 
 static dim3 blocks_of(int T, int tokens_per_wave) { return dim3((unsigned)((T + 4L * tokens_per_wave - 1) / (4L * tokens_per_wave))); }
@@ -423,10 +493,10 @@ extern "C" int32_t dynmo_route_scored(const dynmo_desc* d, const dynmo_route_rul
   if (rc) return rc;
   if (!logits || !expert_idx || !gate_w) return DYNMO_EINVAL;
   if (d->T == 0) return DYNMO_OK;
-  return by_experts(d->E, !misaligned16(logits), [&](auto lpt, auto vpl, auto vec) -> int32_t {
-    constexpr int LPT = decltype(lpt)::value, VPL = decltype(vpl)::value;
+  return by_experts<false>(d->E, !misaligned16(logits), [&](auto lpt, auto, auto vec) -> int32_t {
+    constexpr int LPT = decltype(lpt)::value;
     hipStream_t st = (hipStream_t)stream;
-    DYNMO_TIMED_LAUNCH(K_ROUTE_TOPK, st, route_scored_kernel<LPT, VPL, decltype(vec)::value><<<blocks_of(d->T, 64 / LPT), dim3(256), 0, st>>>(
+    DYNMO_TIMED_LAUNCH(K_ROUTE_TOPK, st, route_scored_kernel<LPT, decltype(vec)::value><<<blocks_of(d->T, 64 / LPT), dim3(256), 0, st>>>(
                                              logits, bias, expert_idx, gate_w, d->T, d->E, d->k, *rule));
     return DYNMO_OK;
   });
@@ -438,7 +508,7 @@ extern "C" int32_t dynmo_route_scored_bwd(const dynmo_desc* d, const dynmo_route
   if (rc) return rc;
   if (!dgate || !logits || !expert_idx || !dlogits) return DYNMO_EINVAL;
   if (d->T == 0) return DYNMO_OK;
-  return by_experts(d->E, !misaligned16(logits, dlogits), [&](auto lpt, auto vpl, auto vec) -> int32_t {
+  return by_experts<true>(d->E, !misaligned16(logits, dlogits), [&](auto lpt, auto vpl, auto vec) -> int32_t {
     constexpr int LPT = decltype(lpt)::value, VPL = decltype(vpl)::value;
     hipStream_t st = (hipStream_t)stream;
     DYNMO_TIMED_LAUNCH(K_ROUTE_TOPK_BWD, st,

@@ -116,6 +116,8 @@ def test_binding_checks_sizes():
     packed = torch.empty(2, B.dynmo_mxfp4_bytes(5, 40), dtype=torch.uint8)
     assert B._mxfp4_sizes(torch.empty(2, 5, 40, dtype=torch.float32), packed) == (2, 5, 40, 0)
     assert B._mxfp4_sizes(torch.empty(5, 40, dtype=torch.bfloat16), packed[0]) == (1, 5, 40, 1)
+    for rows, K in ((1, 8), (16, 128), (17, 136), (100, 512), (33, 1032)):
+        assert B._mxfp4_sizes(torch.empty(rows, K, dtype=torch.float32), torch.empty(B.dynmo_mxfp4_bytes(rows, K), dtype=torch.uint8)) == (1, rows, K, 0)
     for values, p in ((torch.empty(2, 5, 40, dtype=torch.float32), packed[0]), (torch.empty(2, 5, 40, dtype=torch.float32).half(), packed), (torch.empty(40, dtype=torch.float32), packed),
                       (torch.empty(2, 5, 40, dtype=torch.float32), packed.float())):
         with pytest.raises(ValueError):
