@@ -138,6 +138,12 @@ __device__ __forceinline__ u32x4 pack16<bf16_t>(const float* f) {
   return v;
 }
 
+// Between a wavefront's LDS writes and the reads of them by its other lanes: its LDS accesses complete in order, the compiler has to keep it.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 __device__ __forceinline__ float sigmoidf_(float z) { return 1.0f / (1.0f + __expf(-z)); }
 
 }  // namespace dynmo

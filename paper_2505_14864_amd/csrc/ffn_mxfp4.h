@@ -38,10 +38,9 @@ __device__ __forceinline__ f32x4_t mx_mfma(v4i a, v4i b, f32x4_t c, int sa, int 
 
 __device__ __forceinline__ uint2 pack_bf16x4(f32x4_t v) { return {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}; }
 
-// 32 columns from n on, a block of the down product's k, of row block rb: silu(G) U quantised and stored, for this lane's row m (one
-// below `m_end`).  The block lies in two results (16 columns each) and four lanes, so its largest value takes two lane exchanges.
+// 32 columns from n on, a block of the down product's k, of row block rb: silu(G) U quantised and stored.  The block lies in two results (16 columns each) and four lanes, so its largest value takes two lane exchanges.
 // The logistic function uses the hardware's reciprocal (1 ulp): what follows is a grid of eight steps.
-__device__ __forceinline__ void mx_store_swiglu(const MxProduct& p, const f32x4_t (&g)[2], const f32x4_t (&u)[2], int rb, int m, int m_end, int n) {
+__device__ __forceinline__ void mx_store_swiglu(const MxProduct& p, const f32x4_t (&g)[2], const f32x4_t (&u)[2], int rb, int n) {
   const int lane = threadIdx.x & 63, quad = lane >> 4, row = lane & 15;
   const int Fb = mx_k_blocks(p.N), Fq = mx_k_quads(p.N);
   if (n >= Fb * 128) return;
@@ -53,11 +52,6 @@ __device__ __forceinline__ void mx_store_swiglu(const MxProduct& p, const f32x4_
     for (int r = 0; r < 4; ++r) {
       h[c][r] = silu_mul(g[c][r], u[c][r]);
       amax = max(amax, __float_as_uint(h[c][r]) & 0x7fffffffu);
-    }
-    const int col = n + c * 16 + quad * 4;
-    if (p.C0 && m < m_end && col < p.N) {
-      *(uint2*)(p.C0 + (size_t)m * p.N + col) = pack_bf16x4(g[c]);
-      *(uint2*)(p.C1 + (size_t)m * p.N + col) = pack_bf16x4(u[c]);
     }
   }
   amax = max(amax, (uint32_t)__shfl_xor((int)amax, 16, 64));
@@ -73,6 +67,26 @@ __device__ __forceinline__ void mx_store_swiglu(const MxProduct& p, const f32x4_
     *(uint16_t*)(block + c * 8 + quad * 2) = byte == 255 ? (uint16_t)0 : (uint16_t)code;
   }
   if (quad == 0) p.As[((size_t)rb * Fq + n / 512) * kMxScales + (n % 128 / 32 * 16 + row) * 4 + n % 512 / 128] = (char)byte;
+}
+
+// NB results side by side (get(0) .. get(NB - 1), 16 columns each from col0 on) of the sixteen rows from m on, as bfloat16.  They pass through
+// the wavefront's own LDS `patch`, so that a store covers 16 NB columns of a row: from the lanes that have them, 32 bytes of a row each, the stores
+// of 32768 x 4096 results of a sum over 688 took three times what the memory needs (kPatch bytes, 16-byte aligned).
+template <int NB>
+constexpr int kPatch = 16 * (NB * 32 + 16);
+template <int NB, typename Get>
+__device__ __forceinline__ void mx_store_rows(char* patch, bf16_t* C, int N, int m, int m_end, int col0, Get&& get) {
+  constexpr int kPitch = NB * 32 + 16, kLanes = NB * 2, kRows = 64 / kLanes;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int a = 0; a < NB; ++a) *(uint2*)(patch + (lane & 15) * kPitch + a * 32 + (lane >> 4) * 8) = pack_bf16x4(get(a));
+  wave_lds_order();
+#pragma unroll
+  for (int r0 = 0; r0 < 16; r0 += kRows) {
+    const int r = r0 + lane / kLanes, col = col0 + lane % kLanes * 8;
+    if (m + r < m_end && col < N) *(u32x4*)(C + (size_t)(m + r) * N + col) = *(const u32x4*)(patch + r * kPitch + lane % kLanes * 16);
+  }
+  wave_lds_order();
 }
 
 // Which expert's row block (of 16) or row tile: lane e counts those of expert e, `upto` of the experts up to and with e.

@@ -164,24 +164,28 @@ __global__ __launch_bounds__(S::kThreads, 2) void ffn_mx_kernel(const MxProduct 
   else loop(std::integral_constant<int, BT>{});
   wait_stage<0>();  // every load (masked ones included) has landed
 
+  __builtin_amdgcn_s_barrier();
+
   // ---- epilogue
-  const int row = lane & 15;
+  char* const patch = smem + wave * kPatch<GATEUP ? BW / 2 : BW>;
+  static_assert(S::kWaves * kPatch<BW> <= S::kLds, "");
 #pragma unroll
   for (int b = 0; b < BT; ++b) {
     if (b >= my_blocks) break;
-    const int tb = wt + WT * b, m = m0 + tb * 16 + row;
+    const int tb = wt + WT * b, m = m0 + tb * 16;
     if constexpr (GATEUP) {
+      const int n = n0 + ww * (BW / 2) * 16;
+      if (p.C0) {
+        mx_store_rows<BW / 2>(patch, p.C0, p.N, m, m_end, n, [&](int a) { return acc[a][b]; });
+        mx_store_rows<BW / 2>(patch, p.C1, p.N, m, m_end, n, [&](int a) { return acc[BW / 2 + a][b]; });
+      }
 #pragma unroll
       for (int a = 0; a < BW / 2; a += 2) {
         const f32x4_t g2[2] = {acc[a][b], acc[a + 1][b]}, u2[2] = {acc[BW / 2 + a][b], acc[BW / 2 + a + 1][b]};
-        mx_store_swiglu(p, g2, u2, rb0 + tb, m, m_end, n0 + (ww * (BW / 2) + a) * 16);
+        mx_store_swiglu(p, g2, u2, rb0 + tb, n + a * 16);
       }
     } else {
-#pragma unroll
-      for (int a = 0; a < BW; ++a) {
-        const int col = n0 + (ww * BW + a) * 16 + (lane >> 4) * 4;
-        if (m < m_end && col < p.N) *(uint2*)(p.C0 + (size_t)m * p.N + col) = pack_bf16x4(acc[a][b]);
-      }
+      mx_store_rows<BW>(patch, p.C0, p.N, m, m_end, n0 + ww * BW * 16, [&](int a) { return acc[a][b]; });
     }
   }
 }

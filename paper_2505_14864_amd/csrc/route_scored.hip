@@ -26,12 +26,6 @@ constexpr int kMaxRouteExperts = 256;
 // so that a softmax over it has a value.
 __device__ __forceinline__ float clean_logit(float z) { return z != z ? -INFINITY : fminf(z, 3.402823466e38f); }
 
-// Between a wavefront's LDS writes and the reads of them by its other lanes: its LDS accesses complete in order, the compiler has to keep it.
-__device__ __forceinline__ void wave_lds_order() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // The value that the lane has whose place among LPT neighbours is mirrored in one more bit: after log2(LPT) steps of op(v, neighbour)
 // every lane has the result over all of them.
 template <int CTRL>
