@@ -54,18 +54,23 @@ __device__ __forceinline__ void mx_store_swiglu(const MxProduct& p, const f32x4_
       amax = max(amax, __float_as_uint(h[c][r]) & 0x7fffffffu);
     }
   }
-  amax = max(amax, (uint32_t)__shfl_xor((int)amax, 16, 64));
-  amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32, 64));
+  // a swap of two copies leaves both quads of a pair, and both pairs, in every lane
+  auto r = __builtin_amdgcn_permlane16_swap(amax, amax, false, false);
+  amax = max(r[0], r[1]);
+  r = __builtin_amdgcn_permlane32_swap(amax, amax, false, false);
+  amax = max(r[0], r[1]);
   const uint32_t byte = mx_scale_of(amax);
   const float scale = mx_scale_value(byte);
-  char* block = p.A + ((size_t)rb * Fb + n / 128) * kMxTile + n % 128 / 32 * 256 + row * 16;
-#pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    uint32_t code = 0;
-    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, h[c][0], h[c][1], scale, 0);
-    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, h[c][2], h[c][3], scale, 1);
-    *(uint16_t*)(block + c * 8 + quad * 2) = byte == 255 ? (uint16_t)0 : (uint16_t)code;
-  }
+  uint32_t code = 0;  // four codes of each half
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, h[0][0], h[0][1], scale, 0);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, h[0][2], h[0][3], scale, 1);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, h[1][0], h[1][1], scale, 2);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, h[1][2], h[1][3], scale, 3);
+  code = byte == 255 ? 0u : code;
+  // a pair of quads has eight codes of each half: its first quad stores those of the first half, its second those of the other
+  r = __builtin_amdgcn_permlane16_swap(code, code, false, false);
+  const uint32_t word = quad & 1 ? r[0] >> 16 | (r[1] & 0xffff0000u) : (r[0] & 0xffffu) | r[1] << 16;
+  *(uint32_t*)(p.A + ((size_t)rb * Fb + n / 128) * kMxTile + n % 128 / 32 * 256 + row * 16 + (quad & 1) * 8 + (quad >> 1) * 4) = word;
   if (quad == 0) p.As[((size_t)rb * Fq + n / 512) * kMxScales + (n % 128 / 32 * 16 + row) * 4 + n % 512 / 128] = (char)byte;
 }
 
