@@ -49,6 +49,29 @@ __device__ __forceinline__ float over_lanes(float v, Op op) {
   }
   return v;
 }
+// integers in the order of the floating values (no NaN), and back
+__device__ __forceinline__ int order_key(float v) {
+  const int b = __float_as_int(v);
+  return b ^ ((b >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float order_value(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7fffffff)); }
+
+template <int LPT>
+__device__ __forceinline__ int max_over(int v) {
+  v = max(v, __builtin_amdgcn_update_dpp(INT32_MIN, v, 0xB1, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(INT32_MIN, v, 0x4E, 0xf, 0xf, false));
+  if constexpr (LPT >= 16) {
+    v = max(v, __builtin_amdgcn_update_dpp(INT32_MIN, v, 0x141, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(INT32_MIN, v, 0x140, 0xf, 0xf, false));
+  }
+  if constexpr (LPT == 64) {
+    auto r = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+    v = max((int)r[0], (int)r[1]);
+    r = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+    v = max((int)r[0], (int)r[1]);
+  }
+  return v;
+}
 template <int LPT>
 __device__ __forceinline__ float max_over(float v) {
   return over_lanes<LPT>(v, [](float a, float b) { return fmaxf(a, b); });
@@ -244,13 +267,18 @@ __global__ __launch_bounds__(256) void route_scored_kernel(const float* __restri
     if (!(v[q] > -INFINITY) || z[q] == -INFINITY) v[q] = -INFINITY;
     if (fabsf(v[q]) < INFINITY) size = fmaxf(size, fabsf(v[q]));
   }
-  // How far apart two order values a >= b have to be for their order to be that of the 64-bit ones.  A score in 32 bits is off by at most
-  // 2^-21 of the largest (an exponential of a rounded difference, x e^-x of which is at most 0.37, a sum of equal signs, a product), twice for
-  // two and four times to be safe; the sum with the bias by 2^-24 of it, twice, and four times.  By logits: the 64-bit scores have
+  // How far apart two order values have to be for their order to be that of the 64-bit ones, with twice to three times the bound of their
+  // errors.  In units of 2^-24: an exponential is off by 2 and 1.5 |x| relative (the hardware's ulp, the product with log2 e).  The logistic function
+  // of it by 0.25 x 2 + 0.22 x 1.5 for the exponential, whose slope weakens with x, and one each for its sum and its quotient: 2.8, twice for
+  // two values.  A softmax score, of the largest one: 0.37 x 2.5 + 2 for the exponential of a rounded difference, one for the product, and up to 14 for
+  // the common factor: 22 for two.  The sum with the bias: one of its own size, each.  By logits: the 64-bit scores have
   // to differ, too: e^z by 2^-40 relative, and the logistic function, whose slope up to z = 16 is at least 2^-24, by 2^-47; where it is flatter
   // than that, and where both exponentials may vanish, the token is left to the 64 bits.
   const float upper = by_logit && !softmax ? 16.f : INFINITY, lower = by_logit ? (softmax ? top : 0.f) - 600.f : -INFINITY;
-  auto apart = [&](float larger) { return !by_logit ? 0x1p-18f * inv + 0x1p-21f * larger : softmax ? 0x1p-40f * (1.f + larger) : 0x1p-23f; };
+  auto apart = [&](float larger) {
+    if (by_logit) return softmax ? 0x1p-40f * (1.f + larger) : 0x1p-23f;
+    return (softmax ? 0x1p-18f * inv : 0x1p-20f) + 0x1p-22f * larger;
+  };
   bool doubtful = false, doubtful_groups = false;
   if (rule.groups > 1) {
     size = max_over<LPT>(size);
@@ -260,36 +288,43 @@ __global__ __launch_bounds__(256) void route_scored_kernel(const float* __restri
     const float larger = by_logit ? fmaxf(fabsf(least), fabsf(most)) : size;
     doubtful_groups = (most > -INFINITY && !(least - most > 2.f * apart(larger) && least <= upper && least >= lower)) || (!by_logit && !(size < 1e30f));
   }
-  int slot[VPL];
+  // The rounds compare integers in the same order, whose maximum over neighbouring lanes is one instruction.
+  int slot[VPL], key[VPL];
   bool can[VPL];
 #pragma unroll
   for (int q = 0; q < VPL; ++q) {
     slot[q] = -1;
     can[q] = v[q] > -INFINITY;
+    key[q] = order_key(v[q] + 0.f);  // -0 counts as 0
   }
-  float last = NAN, largest = -INFINITY, gap = INFINITY;
+  const int none = order_key(-INFINITY);
+  float last = NAN, before = NAN, largest = -INFINITY, gap = INFINITY;
   int filled = 0;
-  for (int n = 0; n <= k; ++n) {  // one round more: the first that is not chosen
-    float best = v[0];
+  auto round = [&](int n) {
+    int best = key[0];
 #pragma unroll
-    for (int q = 1; q < VPL; ++q) best = fmaxf(best, v[q]);
+    for (int q = 1; q < VPL; ++q) best = max(best, key[q]);
     best = max_over<LPT>(best);
-    if (n == 0) largest = best;
-    if (best > -INFINITY) {
-      gap = fminf(gap, last - best);  // equal infinities leave no gap, but are taken together
-      doubtful = last < lower;
-      last = best;
-      filled = n < k ? n + 1 : filled;
-    }
-    if (n == k) break;
+    const float value = order_value(best);
+    const bool any = best > none;
+    gap = fminf(gap, any ? last - value : INFINITY);  // equal infinities leave no gap, but are taken together
+    before = any ? last : before;
+    last = any ? value : last;
+    if (n == 0) largest = value;
+    return any ? best : INT32_MIN;  // no value has that key
+  };
+  for (int n = 0; n < k; ++n) {
+    const int best = round(n);
+    filled = best != INT32_MIN ? n + 1 : filled;
 #pragma unroll
     for (int q = 0; q < VPL; ++q) {
-      const bool taken = v[q] == best && best > -INFINITY;
+      const bool taken = key[q] == best;
       slot[q] = taken ? n : slot[q];
-      v[q] = taken ? -INFINITY : v[q];
+      key[q] = taken ? none : key[q];
     }
   }
-  doubtful |= filled > 0 && (!(gap > apart(fmaxf(fabsf(largest), fabsf(last)))) || largest > upper);
+  round(k);  // the first that is not chosen
+  doubtful |= filled > 0 && (!(gap > apart(fmaxf(fabsf(largest), fabsf(last)))) || largest > upper || before < lower);
   float total = 0.f, taken = 0.f;
 #pragma unroll
   for (int q = 0; q < VPL; ++q) {
