@@ -27,12 +27,14 @@ std::vector<hipEvent_t> g_free;
 std::mutex g_mu;
 constexpr size_t kMaxPending = 1 << 16;
 
-const char* const kNames[K_COUNT] = {
+const char* const kNames[] = {
     "route_topk",    "route_capacity", "route_active", "route_topk_bwd", "route_capacity_bwd",
     "route_drop",
     "permute_count", "permute_scan",   "permute_scatter", "permute_rows", "permute_bwd",
     "combine",       "combine_bwd",    "ffn_gateup",   "ffn_down",       "ffn_dA",
-    "ffn_dX",        "ffn_dWd",        "ffn_dWg",      "ffn_dWu"};
+    "ffn_dX",        "ffn_dWd",        "ffn_dWg",      "ffn_dWu",
+    "mxfp4_quantize", "mxfp4_dequantize"};
+static_assert(sizeof(kNames) / sizeof(kNames[0]) == K_COUNT, "a name for every role");
 
 hipEvent_t get_event() {
   if (!g_free.empty()) {

@@ -282,6 +282,25 @@ def test_ffn(T, H, F, E, k, counts, gather):
 
 
 @pytest.mark.gpu
+def test_ffn_workspace_at_any_address_and_nothing_written_behind_it():
+    T, H, F, E, k = 20, 264, 136, 3, 2
+    rng = np.random.default_rng(5)
+    packed, _ = make_weights(E, H, F, rng)
+    x = bf16(rng.standard_normal((T * k, H))).cuda()
+    d = B.make_desc(T, H, F, E, k, "bf16")
+    seg = torch.tensor([0, 17, 18, 40], dtype=torch.int32, device="cuda")
+    n = B.dynmo_grouped_ffn_mxfp4_workspace_bytes(d)
+    out = []
+    for at in (0, 1, 255):
+        ws = torch.full((n + 512,), 0x5A, dtype=torch.uint8, device="cuda")
+        y = torch.empty((T * k, H), dtype=torch.bfloat16, device="cuda")
+        B.dynmo_grouped_ffn_mxfp4(d, x, None, seg, *packed, y, None, None, ws[at:at + n])
+        assert (ws[:at] == 0x5A).all() and (ws[at + n:] == 0x5A).all()
+        out.append(y)
+    assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2])
+
+
+@pytest.mark.gpu
 def test_ffn_no_rows_at_all():
     check_ffn(4, 64, 64, 3, 2, [0, 0, 0], True)
 
@@ -391,3 +410,27 @@ def test_ffn_captured_with_two_workspaces():
             ws = torch.empty_like(wss[0])
             B.dynmo_grouped_ffn_mxfp4(d, x, None, seg, *packed, eager, None, None, ws)
             assert torch.equal(eager, y)
+
+
+def test_every_profiled_role_has_a_name():
+    names = [B.dynmo_profile_kernel_name(i) for i in range(B.dynmo_profile_kernel_count())]
+    assert len(set(names)) == len(names) and names[-2:] == ["mxfp4_quantize", "mxfp4_dequantize"]
+
+
+@pytest.mark.gpu
+def test_profiling_sees_the_calls():
+    T, H, F, E, k = 40, 256, 256, 4, 2
+    rng = np.random.default_rng(8)
+    packed, _ = make_weights(E, H, F, rng)
+    layer = RoutedFFNLayer(T, H, F, E, k, "bf16")
+    B.dynmo_profile_reset()
+    B.dynmo_profile_enable(True)
+    try:
+        layer.route_scored(torch.from_numpy(rng.standard_normal((T, E)).astype(np.float32)).cuda(), B.make_rule("sigmoid"))
+        layer.forward_mxfp4(bf16(rng.standard_normal((T, H))).cuda(), *packed)
+    finally:
+        B.dynmo_profile_enable(False)
+    got = {B.dynmo_profile_kernel_name(i): B.dynmo_profile_read(i) for i in range(B.dynmo_profile_kernel_count())}
+    B.dynmo_profile_reset()
+    for name in ("route_topk", "mxfp4_quantize", "ffn_gateup", "ffn_down", "combine"):
+        assert got[name][1] == 1 and got[name][0] > 0, name

@@ -269,6 +269,26 @@ def test_many_tokens_close_to_the_border(score):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("E", [8, 40, 100, 252])
+def test_logits_at_any_address(E):
+    """Rows that start off the 16 bytes that are read at a time: the same results."""
+    T, k = 37, 3
+    g = torch.Generator(device="cuda").manual_seed(E)
+    buf = torch.randn(T * E + 1, generator=g, dtype=torch.float32, device="cuda")
+    d, rule = B.make_desc(T, 8, 8, E, k, "bf16"), B.make_rule("softmax", renormalize=False)
+    got = []
+    for lg in (buf[1:].view(T, E), buf[1:].clone().view(T, E)):
+        ei, gw = torch.empty((T, k), dtype=torch.int32, device="cuda"), torch.empty((T, k), dtype=torch.float32, device="cuda")
+        B.dynmo_route_scored(d, rule, lg, None, ei, gw)
+        out = torch.full((T * E + 2,), 7.0, dtype=torch.float32, device="cuda")
+        dl = out[1:T * E + 1].view(T, E) if lg.data_ptr() % 16 else torch.empty_like(lg)
+        B.dynmo_route_scored_bwd(d, rule, gw, lg, ei, dl)
+        assert out[0] == 7.0 and out[-1] == 7.0
+        got.append((ei, gw, dl))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.gpu
 def test_backward_of_slots_without_an_expert_and_of_one_expert_twice():
     rng = np.random.default_rng(9)
     lg = rng.standard_normal((40, 20)).astype(np.float32)
