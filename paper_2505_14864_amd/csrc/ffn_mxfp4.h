@@ -94,14 +94,15 @@ __device__ __forceinline__ void mx_store_rows(char* patch, bf16_t* C, int N, int
   wave_lds_order();
 }
 
-// Which expert's row block (of 16) or row tile: lane e counts those of expert e, `upto` of the experts up to and with e.
+// Which expert's row block (of 16) or row tile: lane e counts those of expert e, `upto` of the experts up to and with e.  Six additions of
+// neighbouring lanes: the shifts within a row of sixteen, then the rows' last lanes to the rows behind them.
 __device__ __forceinline__ int experts_upto(int count) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(count, d, 64);
-    if (lane >= d) count += o;
-  }
+  count += __builtin_amdgcn_update_dpp(0, count, 0x111, 0xf, 0xf, true);  // row_shr:1, :2, :4, :8
+  count += __builtin_amdgcn_update_dpp(0, count, 0x112, 0xf, 0xf, true);
+  count += __builtin_amdgcn_update_dpp(0, count, 0x114, 0xf, 0xf, true);
+  count += __builtin_amdgcn_update_dpp(0, count, 0x118, 0xf, 0xf, true);
+  count += __builtin_amdgcn_update_dpp(0, count, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
+  count += __builtin_amdgcn_update_dpp(0, count, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
   return count;
 }
 

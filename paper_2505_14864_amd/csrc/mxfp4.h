@@ -33,16 +33,6 @@ __device__ __forceinline__ uint32_t mx_scale_of(uint32_t amax_bits) {
 // 2^(byte - 127); 0 is the subnormal 2^-127
 __device__ __forceinline__ float mx_scale_value(uint32_t byte) { return __uint_as_float(byte == 0 ? 0x00400000u : byte << 23); }
 
-// Eight values / scale -> eight codes, round to nearest even, saturating
-__device__ __forceinline__ uint32_t mx_codes8(const float* v, float scale) {
-  uint32_t c = 0;
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], scale, 0);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], scale, 1);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], scale, 2);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], scale, 3);
-  return c;
-}
-
 // mxfp4.hip.  Quantises the rows of the expert segments for the grouped products: row block b of the result holds sixteen rows of one
 // expert (an expert's last block fewer), the experts' blocks one after another; `gather`: row p is x[gather[p] / gather_div], or nullptr.
 int32_t mx_quantize_segments(const dynmo_desc* d, const void* x, const int32_t* gather, const int32_t* seg, int K, void* codes, void* scales,

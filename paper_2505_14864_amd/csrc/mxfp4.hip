@@ -24,15 +24,41 @@ __device__ __forceinline__ void load8(const T* p, int left, u32x4* v) {
 __device__ __forceinline__ uint32_t quad_xor1(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true); }
 __device__ __forceinline__ uint32_t quad_xor2(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true); }
 
-// Eight values of each lane -> their codes, and the block's scale byte (the same in the four lanes of a block)
-__device__ __forceinline__ uint32_t quantize_block(const float* v, uint32_t* scale) {
+// Eight values of each lane -> their codes, and the block's scale byte (the same in the four lanes of a block).  Of bfloat16 values the largest
+// magnitude is found on pairs, and the conversion takes them as they are.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+template <typename T>
+__device__ __forceinline__ uint32_t quantize_block(const u32x4* piece, uint32_t* scale) {
   uint32_t amax = 0;
+  if constexpr (sizeof(T) == 2) {
+    u16x2 two = {0, 0};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(v[i]) & 0x7fffffffu);
+    for (int i = 0; i < 4; ++i) two = __builtin_elementwise_max(two, __builtin_bit_cast(u16x2, piece[0][i] & 0x7fff7fffu));
+    amax = (uint32_t)max(two.x, two.y) << 16;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = max(amax, piece[i / 4][i % 4] & 0x7fffffffu);
+  }
   amax = max(amax, quad_xor1(amax));
   amax = max(amax, quad_xor2(amax));
   *scale = mx_scale_of(amax);
-  return *scale == 255 ? 0u : mx_codes8(v, mx_scale_value(*scale));
+  const float unit = mx_scale_value(*scale);
+  uint32_t c = 0;
+  if constexpr (sizeof(T) == 2) {
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2_t, (uint32_t)piece[0].x), unit, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2_t, (uint32_t)piece[0].y), unit, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2_t, (uint32_t)piece[0].z), unit, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2_t, (uint32_t)piece[0].w), unit, 3);
+  } else {
+    float v[8];
+    unpack16<float>(piece[0], v);
+    unpack16<float>(piece[1], v + 4);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], unit, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], unit, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], unit, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], unit, 3);
+  }
+  return *scale == 255 ? 0u : c;
 }
 
 // Tiles first, first + stride, .. of a row block.  src[i]: this lane's row 4 i + lane / 16 of it, or nullptr.
@@ -59,10 +85,7 @@ __device__ __forceinline__ void quantize_rows(const T* const (&src)[4], int K, i
       const int r = 4 * i + (lane >> 4);
       uint32_t scale = 0;
       if (kb < Kb) {
-        float v[8];
-#pragma unroll
-        for (int c = 0; c < kPieces; ++c) unpack16<T>(now[i][c], v + c * Elem<T>::kVec);
-        *(uint32_t*)(codes + (size_t)kb * kMxTile + g * 256 + r * 16 + (lane & 3) * 4) = quantize_block(v, &scale);
+        *(uint32_t*)(codes + (size_t)kb * kMxTile + g * 256 + r * 16 + (lane & 3) * 4) = quantize_block<T>(now[i], &scale);
       }
       if ((lane & 3) == 0) scales[(size_t)(kb / 4) * kMxScales + (g * 16 + r) * 4 + kb % 4] = (char)scale;
     }
