@@ -127,14 +127,14 @@ int32_t dynmo_route_topk_all_bwd(const dynmo_desc* d, const float* dgate, const 
  *   groups > 1: the experts are `groups` equal runs of indices; a group counts the sum of its group_best (1 or 2) largest v, and
  *     only the experts of the top_groups groups that count most can be chosen
  *   slot s gets the expert with the s-th largest v of those that can be chosen
- *   gate_w = s of the chosen expert, divided by the sum over the chosen ones if renormalize is 1 (zero where that sum is),
+ *   gate_w = s of the chosen expert, divided by the sum over the chosen ones if renormalize is 1 (also where all of them are tiny),
  *     times scale
  * Equal values: lower index first, groups as experts.  v is compared in 64 bits, from scores computed in 64 bits.  The bias
  * steers the selection only.
  * An expert whose logit is NaN or -inf, or whose v is, is never chosen, and its score is zero; a logit of +inf counts as the
  * largest finite number.  A slot for which no expert is left gets expert_idx -1 and gate_w 0 (a group with fewer than
  * group_best experts that can be chosen counts those it has).
- * Needs E a multiple of groups, 1 <= top_groups <= groups and k <= top_groups * (E / groups); E up to 256 here, for a caller
+ * Needs E a multiple of groups, 1 <= top_groups <= groups and k <= top_groups * (E / groups), T below 2^26; E up to 256 here, for a caller
  * who routes over the experts of several workers and maps the indices to its own (and to -1) before dynmo_permute.
  * logits [T,E] -> expert_idx [T,k], gate_w [T,k].
  *
@@ -303,7 +303,7 @@ int32_t dynmo_grouped_ffn_kernel(const dynmo_desc* d, int32_t product);
  * calls.  Matrices follow one another without gaps: src [n, rows, K] -> packed [n, dynmo_mxfp4_bytes(rows, K)].
  *
  * dynmo_mxfp4_quantize: float or bfloat16 -> packed; dynmo_mxfp4_dequantize: packed -> the values it stands for, exact in either
- * type.  K must be a multiple of 8 (DYNMO_BF16) or 4 (DYNMO_F32), and n * ceil(rows / 16) * ceil(K / 512) below 2^31 (DYNMO_EUNSUPPORTED).
+ * type.  K must be a multiple of 8 (DYNMO_BF16) or 4 (DYNMO_F32), and n * ceil(rows / 16) * ceil(K / 512) below 2^24 (DYNMO_EUNSUPPORTED).
  * Quantising what dequantising gave returns the same values, so a checkpoint in another order of the same format loses nothing. */
 size_t dynmo_mxfp4_bytes(int32_t rows, int32_t K);
 int32_t dynmo_mxfp4_quantize(int32_t n, int32_t rows, int32_t K, int32_t dtype, const void* src, void* packed, void* stream);
@@ -313,7 +313,8 @@ size_t dynmo_grouped_ffn_mxfp4_workspace_bytes(const dynmo_desc* d);
 
 /* dynmo_grouped_ffn_fwd on packed weights: with Q the quantisation above, along a row,
  * G = Q(X) Wg[e]^T, U = Q(X) Wu[e]^T, A = Q(silu(G) * U), Y = A Wd[e]^T; products of 4-bit values on the matrix cores, fp32 sums, G, U and A kept in
- * fp32 up to A's quantisation.  DYNMO_BF16 only (X, Y and the saved G, U bfloat16), H and F up to 2^22.
+ * fp32 up to A's quantisation.  DYNMO_BF16 only (X, Y and the saved G, U bfloat16), H and F up to 2^22, and
+ * (T*k / 128 + min(E, T*k)) * max(F, H) / 64 up to 2^23 (DYNMO_EUNSUPPORTED where that leaves too many tiles for a launch).
  * src_slot NULL: x is x_p [T*k,H], expert-sorted rows; else x [T,H] in token order, row p being x[src_slot[p] / k] as for
  * dynmo_grouped_ffn_fwd_gather (of any size).  Wg, Wu [E, dynmo_mxfp4_bytes(F, H)], Wd [E, dynmo_mxfp4_bytes(H, F)].
  * G_save, U_save [T*k,F]: both, or both NULL.  With them, and with the weights dequantised to bfloat16,

@@ -159,11 +159,24 @@ def route_scores(logits, score):
     return out, dead
 
 
+def _score_shares(z, score):
+    """s / sum(s) of one token's chosen experts from their logits (finite), without forming scores that may vanish: relative to e^m."""
+    z = _f64(np.minimum(np.asarray(z, dtype=np.float32), np.finfo(np.float32).max))
+    if z.size == 0:
+        return z
+    if score == "softmax":
+        r = np.exp(z - z.max())
+    else:  # log s = min(z, 0) - log(1 + e^-|z|)
+        log_s = np.minimum(z, 0.0) - np.log1p(np.exp(-np.abs(z)))
+        r = np.exp(log_s - log_s.max())
+    return r / r.sum()
+
+
 def route_scored(logits, bias, k, score="softmax", groups=1, top_groups=1, group_best=1, renormalize=True, scale=1.0):
     """Token-choice routing by scores with a selection bias and expert groups (the balancing without an auxiliary loss
     that Sec. 2.1 names, and the restriction of a token to few workers' experts).  Order value v = score + bias in float64;
     a group counts the sum of its group_best largest v (those it has); of the top_groups groups' experts the k with the
-    largest v, ties to the lower index; weights are the chosen scores, divided by their sum if renormalize, times scale.
+    largest v, ties to the lower index; weights are the chosen scores, divided by their sum if renormalize (also where they vanish in 64 bits), times scale.
     Experts whose logit is NaN or -inf, or whose v is, are never chosen; a slot without an expert is -1 with weight 0.
     Returns expert_idx int32 [T, k], gate_w f64 [T, k]."""
     s, dead = route_scores(logits, score)
@@ -182,9 +195,7 @@ def route_scored(logits, bias, k, score="softmax", groups=1, top_groups=1, group
         stay = sorted(range(groups), key=lambda g: (-worth[g], g))[:top_groups]
         order = sorted((e for e in can if e // size in stay), key=lambda e: (-v[t, e], e))[:k]
         idx[t, :len(order)] = order
-        w = s[t, order]
-        if renormalize:
-            w = w / w.sum() if w.sum() > 0 else np.zeros_like(w)
+        w = _score_shares(np.asarray(logits)[t, order], score) if renormalize else s[t, order]
         gate[t, :len(order)] = w * F64(np.float32(scale))
     return idx, gate
 
@@ -197,16 +208,17 @@ def route_scored_bwd(dgate, logits, expert_idx, score="softmax", renormalize=Tru
     out = np.zeros((T, E), F64)
     for t in range(T):
         slots = [j for j in range(ei.shape[1]) if 0 <= ei[t, j] < E]
-        p = s[t, ei[t, slots]]
         g = _f64(dgate)[t, slots] * F64(np.float32(scale))
-        if renormalize:
-            total = p.sum()
-            if total > 0:  # d(p_i / S) / dp_j = delta_ij / S - p_i / S^2, contracted over i
-                g = (np.eye(len(slots)) / total - np.outer(p, np.ones(len(slots))) / total ** 2).T @ g
-            else:
-                g = np.zeros_like(g)
+        chosen = ei[t, slots]
+        if renormalize:  # d w_i / d z_j = w_i (delta_ij - w_j) s'_j / s_j with s' / s = 1 (softmax: its other terms cancel) or 1 - s
+            live = ~np.isnan(np.asarray(logits)[t, chosen]) & (np.asarray(logits)[t, chosen] != -np.inf)
+            w = np.zeros(len(slots), F64)
+            w[live] = _score_shares(np.asarray(logits)[t, chosen[live]], score)
+            d = (np.diag(w) - np.outer(w, w)).T @ g
+            np.add.at(out[t], chosen, d if score == "softmax" else d * (1.0 - s[t, chosen]))
+            continue
         ds = np.zeros(E, F64)
-        np.add.at(ds, ei[t, slots], g)
+        np.add.at(ds, chosen, g)
         out[t] = ds * s[t] * (1.0 - s[t]) if score == "sigmoid" else s[t] * (ds - (ds * s[t]).sum())
     return out
 

@@ -4,11 +4,21 @@
 //   G = Q(X) Wg^T, U = Q(X) Wu^T, A = Q(silu(G) U), Y = A Wd^T
 //
 // G, U and A are fp32 values up to A's quantisation: rounding them to bf16 in between would move values over the borders of a
-// four-bit grid that has eight steps.  Operand A of an MFMA is the weights and operand B the rows, so that a lane of the result holds four consecutive columns
-// of one row, and a block of 32 columns lies in two results and four lanes: its largest value takes two lane exchanges.
+// four-bit grid that has eight steps.  Saved G and U, and Y, are rounded to bf16 once.
 //
-// One workgroup of four wavefronts (2 x 2) per output tile of 128 weight rows x 128 rows, k in steps of 128 through a ring of three LDS
-// stages; a step's tiles of 1 KB are loaded into LDS as they lie in memory.
+// One workgroup of four wavefronts (2 x 2) per output tile of 128 or 256 weight rows x 128 rows; the hardware deals them, and three (two) of them share a
+// compute unit, so that one's prologue, waits and epilogue run under the others' matrix instructions.  k goes in steps of 128 through a ring of three
+// LDS stages: a step's tiles of 1 KB are loaded into LDS as they lie in memory and read from there without bank conflicts (counted: none); the
+// scales of four steps come with every fourth.  A load has a descriptor that stays and a scalar offset that moves: with addresses worked
+// out per load the scalar instructions took 15 % (gate/up of 8192 rows 686 -> 600 us).
+//
+// Bound, 8192 rows over 8 experts, 4096 x 14336: gate/up 3.6 PFLOP/s, down 3.4, of 6.5 to 7 that the instruction alone reaches on random operands from
+// registers.  Both are held by the chip's power: the clock is at 1.76 GHz here, and the same launches on operands of zeros take 443 and 233
+// us instead of 590 and 291.  What is left at that is the loads (447 and 202 us without them, 355 and 234 without the matrix instructions and
+// the reads).  Measured and no faster: tiles of 256 x 256 by eight wavefronts (603, 324) or by four of 128 x 128 (667, 330), 128 x 256 (595, 293), the next
+// step's operands read from LDS during the present one (609, 304), row tiles walked in chunks of 8, 12 or 16.  Two stages instead of three: down of 256
+// rows 51 -> 83 us; four: a workgroup less per compute unit, gate/up of 64 ragged experts 67 -> 75, of 2000 rows 165 -> 215.
+// Few rows: bound by reading the weights once (64 rows over 8 experts, gate/up 84 us, 6 TB/s).
 #include "ffn_mxfp4.h"
 
 namespace dynmo {
@@ -201,7 +211,7 @@ template <bool GATEUP, class S>
 static int32_t launch_mx(MxProduct p, const dynmo_desc* d, KernelId id, hipStream_t st) {
   const int64_t tiles = mx_tile_count<GATEUP, S>(p, d);
   if (tiles == 0) return DYNMO_OK;
-  if (tiles > (1 << 30)) return DYNMO_EUNSUPPORTED;
+  if (tiles > (1 << 24) - (1 << 12)) return DYNMO_EUNSUPPORTED;  // a launch has fewer than 2^32 threads; the list is rounded up to whole runs
   p.list = tile_list((int)tiles);
   DYNMO_TIMED_LAUNCH(id, st, ffn_mx_kernel<GATEUP, S><<<dim3(p.list.blocks), dim3(S::kThreads), 0, st>>>(p));
   return DYNMO_OK;

@@ -10,13 +10,16 @@ namespace dynmo {
 // contiguous bytes of four rows, and a store 64 bytes of each block column.  The four wavefronts of a workgroup share a row block.
 constexpr int kQuantThreads = 256, kQuantWaves = 4;
 
-template <typename T>
+// ONCE: past the caches.  A tensor that is quantised is read once, and what it would push out of them is its packed form, which is used next; rows
+// that are gathered are read as often as they have experts.  (8 x 14336 x 4096 in fp32 and back, us: loads and stores past the caches 427 + 404,
+// the stores only 406 + 495, neither 439 + 492; gathered rows, 8 times each: 22 past the caches, 16.)
+template <bool ONCE, typename T>
 __device__ __forceinline__ void load8(const T* p, int left, u32x4* v) {
   constexpr int kVec = Elem<T>::kVec;
 #pragma unroll
   for (int i = 0; i < 8 / kVec; ++i) {
     v[i] = u32x4{0u, 0u, 0u, 0u};
-    if (i * kVec < left) v[i] = *(const u32x4*)(p + i * kVec);
+    if (i * kVec < left) v[i] = ONCE ? __builtin_nontemporal_load((const u32x4*)(p + i * kVec)) : *(const u32x4*)(p + i * kVec);
   }
 }
 
@@ -62,7 +65,7 @@ __device__ __forceinline__ uint32_t quantize_block(const u32x4* piece, uint32_t*
 }
 
 // Tiles first, first + stride, .. of a row block.  src[i]: this lane's row 4 i + lane / 16 of it, or nullptr.
-template <typename T>
+template <bool ONCE, typename T>
 __device__ __forceinline__ void quantize_rows(const T* const (&src)[4], int K, int first, int stride, char* codes, char* scales) {
   constexpr int kPieces = 8 / Elem<T>::kVec;
   const int lane = threadIdx.x & 63, g = (lane & 15) >> 2, Kb = mx_k_blocks(K), tiles = mx_k_quads(K) * 4;
@@ -70,7 +73,7 @@ __device__ __forceinline__ void quantize_rows(const T* const (&src)[4], int K, i
   auto load = [&](int kb) {
     const int k = kb * 128 + (lane & 15) * 8;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load8<T>(src[i] + k, src[i] ? K - k : 0, next[i]);
+    for (int i = 0; i < 4; ++i) load8<ONCE>(src[i] + k, src[i] ? K - k : 0, next[i]);
   };
   load(first);
   for (int kb = first; kb < tiles; kb += stride) {  // tiles from Kb on have scales (zero) only
@@ -105,13 +108,12 @@ __global__ __launch_bounds__(kQuantThreads) void mx_quantize_kernel(const T* __r
     const int r = rb * 16 + 4 * i + (lane >> 4);
     row[i] = r < rows ? src + (m * rows + r) * (long)K : nullptr;
   }
-  quantize_rows<T>(row, K, part * kQuantWaves + (threadIdx.x >> 6), parts * kQuantWaves, matrix + (size_t)rb * Kb * kMxTile,
+  quantize_rows<true>(row, K, part * kQuantWaves + (threadIdx.x >> 6), parts * kQuantWaves, matrix + (size_t)rb * Kb * kMxTile,
                    matrix + mx_code_bytes(Rb, K) + (size_t)rb * Kq * kMxScales);
 }
 
 // Values four at a time: a store of the wavefront covers the 128 values of two rows (fp32: 512 contiguous bytes each).  The stores
-// go past the caches, which is what the memory takes faster where the values are more than they hold (8 x 14336 x 4096 in fp32 492 -> 399 us,
-// 5.3 TB/s) and costs nothing where they are not (1003 x 1032).  Quantising: 430 us, 4.9 TB/s.
+// go past the caches (figures at load8); of 1003 x 1032 bf16 values 4.2 us either way.
 template <typename T>
 __global__ __launch_bounds__(kQuantThreads) void mx_dequantize_kernel(const char* __restrict__ packed, T* __restrict__ dst, int rows, int K) {
   const int Kb = mx_k_blocks(K), Kq = mx_k_quads(K), Rb = mx_row_blocks(rows);
@@ -165,9 +167,11 @@ __global__ __launch_bounds__(kQuantThreads) void mx_quantize_segments_kernel(con
     const int p = first + 4 * i + (lane >> 4);
     row[i] = p < last ? x + (size_t)(gather ? gather[p] / gather_div : p) * K : nullptr;
   }
-  quantize_rows<T>(row, K, part * kQuantWaves + (threadIdx.x >> 6), parts * kQuantWaves, codes + (size_t)rb * Kb * kMxTile,
+  quantize_rows<false>(row, K, part * kQuantWaves + (threadIdx.x >> 6), parts * kQuantWaves, codes + (size_t)rb * Kb * kMxTile,
                    scales + (size_t)rb * Kq * kMxScales);
 }
+
+constexpr int64_t kMaxBlocks = 1 << 24;  // of 256 threads: a launch has fewer than 2^32
 
 // Workgroups per row block: as many as the block has tiles for, but no more than some eight per compute unit in all.
 static int parts_of(int64_t row_blocks, int K) {
@@ -179,6 +183,7 @@ int32_t mx_quantize_segments(const dynmo_desc* d, const void* x, const int32_t* 
                              hipStream_t st) {
   const int64_t row_blocks = mx_max_row_blocks(d);
   if (row_blocks == 0) return DYNMO_OK;
+  if (row_blocks >= kMaxBlocks) return DYNMO_EUNSUPPORTED;
   const int parts = parts_of(row_blocks, K);
   DYNMO_TIMED_LAUNCH(K_MXFP4_QUANTIZE, st, mx_quantize_segments_kernel<bf16_t><<<dim3((unsigned)(row_blocks * parts)), dim3(kQuantThreads), 0, st>>>(
                                                (const bf16_t*)x, gather, d->k, seg, d->E, K, parts, (char*)codes, (char*)scales));
@@ -190,7 +195,7 @@ static int32_t check_matrix(int32_t n, int32_t rows, int32_t K, int32_t dtype, c
   if (K % (dtype == DYNMO_BF16 ? 8 : 4)) return DYNMO_EUNSUPPORTED;  // rows move in 16-byte pieces
   if (K > 0x7fffffff - 512 || rows > 0x7fffffff - 16) return DYNMO_EUNSUPPORTED;
   const __int128 all = (__int128)n * mx_row_blocks(rows) * mx_k_quads(K);
-  if (all > 0x7fffffff) return DYNMO_EUNSUPPORTED;
+  if (all >= kMaxBlocks) return DYNMO_EUNSUPPORTED;
   *blocks = (int64_t)all;
   if (*blocks == 0) return DYNMO_OK;
   if (!values || !packed || misaligned16(values, packed)) return DYNMO_EINVAL;

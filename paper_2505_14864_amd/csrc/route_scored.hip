@@ -380,18 +380,29 @@ __global__ __launch_bounds__(256) void route_scored_kernel(const float* __restri
         v64[q] = mine ? -INFINITY : v64[q];
       }
     }
-    double total64 = 0.0;
+    double total64 = 1.0;
+    if (rule.renormalize) {  // relative to the largest chosen score (of a sigmoid, to e^z of it where that is below one): they may all be tiny
+      float m = -INFINITY;
 #pragma unroll
-    for (int q = 0; q < VPL; ++q) total64 += slot64[q] >= 0 ? s64[q] : 0.0;
+      for (int q = 0; q < VPL; ++q) m = slot64[q] >= 0 ? fmaxf(m, z[q]) : m;
+      m = max_over<LPT>(m);
+      if (!softmax) m = fminf(m, 0.f);
+      total64 = 0.0;
 #pragma unroll
-    for (int m = 1; m < LPT; m <<= 1) total64 += __shfl_xor(total64, m, 64);
-    const double over64 = rule.renormalize && total64 > 0.0 ? total64 : 1.0;  // divided by: it may be subnormal (or zero, as all its terms are)
+      for (int q = 0; q < VPL; ++q) {
+        const double up = softmax || z[q] <= 0.f ? exp((double)z[q] - (double)m) : 1.0;
+        s64[q] = slot64[q] >= 0 ? (softmax ? up : up / (1.0 + exp(-fabs((double)z[q])))) : 0.0;
+        total64 += s64[q];
+      }
+#pragma unroll
+      for (int n = 1; n < LPT; n <<= 1) total64 += __shfl_xor(total64, n, 64);
+    }
     if (sum_over<LPT>(doubtful ? 1.f : 0.f) > 0.f) {
       filled = filled64;
 #pragma unroll
       for (int q = 0; q < VPL; ++q) {
         slot[q] = slot64[q];
-        s[q] = (float)(s64[q] / over64 * rule.scale);
+        s[q] = (float)(s64[q] / total64 * rule.scale);  // of tokens with a chosen expert; others have nothing to store
       }
     }
   }
@@ -408,10 +419,14 @@ __global__ __launch_bounds__(256) void route_scored_kernel(const float* __restri
   }
 }
 
-// ds_j = (g_j - sum_i g_i s_i / S) / S with S the sum of the chosen scores (or g_j), g = dgate * scale; then through the scores:
-// sigmoid ds s (1 - s) at the chosen experts, softmax p_e ([e chosen] ds_e - sum_j ds_j p_j) everywhere.
-// Bound by memory: the sigmoid reads the chosen logits only.  The slots' gradients meet their experts in an LDS row per token, slot after
-// slot, so that an expert in several slots gets their sum in a fixed order.
+// With g = dgate * scale, s the chosen scores and w = s / sum s:
+//   renormalised         dlogit_j = w_j (g_j - sum_i g_i w_i), for the sigmoid times 1 - s_j: at the chosen experts, zero elsewhere
+//   sigmoid as it is     dlogit_j = g_j s_j (1 - s_j)
+//   softmax as it is     dlogit_e = p_e ([e chosen] g_e - sum_i g_i p_i)
+// Only the last one needs more than the chosen logits.  The w are taken relative to the largest chosen score (of a sigmoid, to e^z of it where that is
+// below one): the chosen ones may lie far below the rest, kept up by the bias.
+// Bound by memory.  The slots' gradients meet their experts in an LDS row per token, slot after slot, so that an expert in several
+// slots gets their sum in a fixed order.
 template <int LPT, int VPL, bool VEC>
 __global__ __launch_bounds__(256) void route_scored_bwd_kernel(const float* __restrict__ dgate, const float* __restrict__ logits,
                                                                const int32_t* __restrict__ expert_idx, float* __restrict__ dlogits,
@@ -420,49 +435,64 @@ __global__ __launch_bounds__(256) void route_scored_bwd_kernel(const float* __re
   __shared__ __attribute__((aligned(16))) float grads[4][kTokens][LPT * VPL];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane % LPT, tok = lane / LPT;
   const long t = ((long)blockIdx.x * 4 + wave) * kTokens + tok;
-  const bool live = t < T, softmax = rule.score == DYNMO_SCORE_SOFTMAX;
+  const bool live = t < T, softmax = rule.score == DYNMO_SCORE_SOFTMAX, all = softmax && !rule.renormalize;
   float* const row = grads[wave][tok];
   const float* const lg = logits + t * E;
   float z[VPL], s[VPL], top = 0.f, inv = 1.f;
-  if (softmax) {
+  if (all) {
     load_logits<LPT, VPL, VEC>(lg, j, E, live, z);
     scores32<LPT, VPL>(rule.score, z, s, &top, &inv);
   }
 #pragma unroll
   for (int q = 0; q < VPL; q += 4) *(u32x4*)(row + expert_of<LPT>(q, j)) = u32x4{0u, 0u, 0u, 0u};
   wave_lds_order();
-  // slot `n` of the token: its expert (-1: none), that expert's score, the slope of the logistic function there, and the gradient
-  auto slot = [&](int n, float* score, float* slope, float* g) {
-    *score = *slope = *g = 0.f;
+  // slot `n` of the token: its expert (-1: none), that expert's logit and the gradient
+  auto slot = [&](int n, float* x, float* g) {
+    *x = -INFINITY;
+    *g = 0.f;
     if (!live || n >= k) return -1;
     const int e = expert_idx[t * k + n];
     if (e < 0 || e >= E) return -1;
-    const float x = clean_logit(lg[e]);
-    *score = softmax ? (x == -INFINITY ? 0.f : __expf(x - top) * inv) : sigmoidf_(x);
-    *slope = softmax ? 1.f : *score * sigmoidf_(-x);
+    *x = clean_logit(lg[e]);
     *g = dgate[t * k + n] * rule.scale;
     return e;
   };
-  float total = 0.f, inner = 0.f, score, slope, g;
-  int e = -1;
+  float x, g;
+  int e = slot(j, &x, &g);  // with more slots than lanes they are looked up again
+  if (rule.renormalize) {
+    top = x;
+    for (int n = j + LPT; n < k; n += LPT) {
+      slot(n, &x, &g);
+      top = fmaxf(top, x);
+    }
+    top = max_over<LPT>(top);
+    if (!softmax) top = fminf(top, 0.f);
+  }
+  auto score = [&](float v) {  // in units of e^top (not all: 1)
+    if (v == -INFINITY) return 0.f;
+    if (softmax) return __expf(v - top) * inv;
+    return v > 0.f ? sigmoidf_(v) : __expf(v - top) * sigmoidf_(-v);
+  };
+  float total = 0.f, inner = 0.f;
   for (int n = j; n < k; n += LPT) {
-    e = slot(n, &score, &slope, &g);
-    total += score;
-    inner += g * score;
+    if (k > LPT) slot(n, &x, &g);
+    total += score(x);
+    inner += g * score(x);
   }
   total = sum_over<LPT>(total);
   inner = sum_over<LPT>(inner);
-  const float by = total > 0.f ? 1.f / total : 0.f;
+  const float by = !rule.renormalize ? 1.f : total > 0.f ? 1.f / total : 0.f;
   for (int base = 0; base < k; base += LPT) {
-    if (k > LPT || j >= k) e = slot(base + j, &score, &slope, &g);  // else it is still there
-    const float ds = (rule.renormalize ? (g - inner * by) * by : g) * slope;
+    if (k > LPT) e = slot(base + j, &x, &g);
+    float d = g;  // all: what the expert's own score is multiplied with below
+    if (!all) d = score(x) * by * (rule.renormalize ? g - inner * by : g) * (softmax ? 1.f : sigmoidf_(-x));
+    if (!all && x == -INFINITY) d = 0.f;
     for (int i = 0; i < LPT && base + i < k; ++i) {
-      if (j == i && e >= 0) __hip_atomic_fetch_add(row + e, ds, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+      if (j == i && e >= 0) __hip_atomic_fetch_add(row + e, d, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
       wave_lds_order();
     }
   }
   wave_lds_order();
-  if (rule.renormalize) inner = 0.f;  // sum_j ds_j s_j
   if (!live) return;
   float* const out = dlogits + t * E;
 #pragma unroll
@@ -470,7 +500,7 @@ __global__ __launch_bounds__(256) void route_scored_bwd_kernel(const float* __re
     const int at = expert_of<LPT>(q, j);
     float d[4];
     unpack16<float>(*(const u32x4*)(row + at), d);
-    if (softmax) {
+    if (all) {
 #pragma unroll
       for (int c = 0; c < 4; ++c) d[c] = s[q + c] * (d[c] - inner);
     }
@@ -489,6 +519,7 @@ static int32_t check_route(const dynmo_desc* d, const dynmo_route_rule* r) {
   if (rc) return rc;
   if (!r || (r->score != DYNMO_SCORE_SOFTMAX && r->score != DYNMO_SCORE_SIGMOID)) return DYNMO_EINVAL;
   if (r->groups < 1 || d->E % r->groups || r->top_groups < 1 || r->top_groups > r->groups) return DYNMO_EINVAL;
+  if (d->T >= 1 << 26) return DYNMO_EUNSUPPORTED;  // 2^24 workgroups of four tokens: a launch has fewer than 2^32 threads
   if (r->group_best < 1 || r->group_best > 2 || (r->renormalize != 0 && r->renormalize != 1)) return DYNMO_EINVAL;
   if (!(r->scale - r->scale == 0.f)) return DYNMO_EINVAL;                  // NaN or infinite
   if (d->k > r->top_groups * (d->E / r->groups)) return DYNMO_EINVAL;  // more slots than experts that can be chosen
@@ -510,7 +541,7 @@ static int32_t by_experts(int E, bool aligned, F&& f) {
   else return with(integral_constant<int, 16>{}, integral_constant<int, 16>{});
 }
 
-static dim3 blocks_of(int T, int tokens_per_wave) { return dim3((unsigned)((T + 4L * tokens_per_wave - 1) / (4L * tokens_per_wave))); }
+static unsigned blocks_of(int T, int tokens_per_wave) { return (unsigned)((T + 4L * tokens_per_wave - 1) / (4L * tokens_per_wave)); }
 
 }  // namespace dynmo
 
@@ -525,7 +556,7 @@ extern "C" int32_t dynmo_route_scored(const dynmo_desc* d, const dynmo_route_rul
   return by_experts<false>(d->E, !misaligned16(logits), [&](auto lpt, auto, auto vec) -> int32_t {
     constexpr int LPT = decltype(lpt)::value;
     hipStream_t st = (hipStream_t)stream;
-    DYNMO_TIMED_LAUNCH(K_ROUTE_TOPK, st, route_scored_kernel<LPT, decltype(vec)::value><<<blocks_of(d->T, 64 / LPT), dim3(256), 0, st>>>(
+    DYNMO_TIMED_LAUNCH(K_ROUTE_TOPK, st, route_scored_kernel<LPT, decltype(vec)::value><<<dim3(blocks_of(d->T, 64 / LPT)), dim3(256), 0, st>>>(
                                              logits, bias, expert_idx, gate_w, d->T, d->E, d->k, *rule));
     return DYNMO_OK;
   });
@@ -541,7 +572,7 @@ extern "C" int32_t dynmo_route_scored_bwd(const dynmo_desc* d, const dynmo_route
     constexpr int LPT = decltype(lpt)::value, VPL = decltype(vpl)::value;
     hipStream_t st = (hipStream_t)stream;
     DYNMO_TIMED_LAUNCH(K_ROUTE_TOPK_BWD, st,
-                       route_scored_bwd_kernel<LPT, VPL, decltype(vec)::value><<<blocks_of(d->T, 64 / LPT), dim3(256), 0, st>>>(
+                       route_scored_bwd_kernel<LPT, VPL, decltype(vec)::value><<<dim3(blocks_of(d->T, 64 / LPT)), dim3(256), 0, st>>>(
                            dgate, logits, expert_idx, dlogits, d->T, d->E, d->k, *rule));
     return DYNMO_OK;
   });

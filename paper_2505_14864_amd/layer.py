@@ -97,10 +97,12 @@ class RoutedFFNLayer:
         B.dynmo_route_scored(self.d, rule, logits, bias, self.expert_idx, self.gate_w)
 
     def route_capacity(self, scores, cap):
+        self._rule = None
         Bn, S = scores.shape
         B.dynmo_route_capacity(self.d, scores, Bn, S, cap, self.expert_idx, self.gate_w)
 
     def route_active(self, exit_layer, layer):
+        self._rule = None
         B.dynmo_route_active(self.d, exit_layer, layer, self.expert_idx, self.gate_w)
 
     # ---- forward / backward after routing ----

@@ -90,7 +90,7 @@ def test_refusals_without_a_gpu():
         assert call(1, -4, 8, 1, 16, 16, None) == -1 and call(1, 4, 0, 1, 16, 16, None) == -1
         assert call(1, 4, 12, 1, 16, 16, None) == -2 and call(1, 4, 6, 0, 16, 16, None) == -2
         assert call(1, 4, 8, 1, 16, 24, None) == -1 and call(1, 4, 8, 1, 24, 16, None) == -1
-        assert call(1 << 20, 1 << 20, 8, 1, 16, 16, None) == -2
+        assert call(1 << 20, 1 << 20, 8, 1, 16, 16, None) == -2 and call(1, 1 << 28, 8, 1, 16, 16, None) == -2
         assert call(0, 4, 8, 1, None, None, None) == 0 and call(3, 0, 8, 1, None, None, None) == 0
     ffn, big = lib.dynmo_grouped_ffn_mxfp4, 1 << 40
     d = B.make_desc(8, 16, 16, 4, 2, "bf16")
@@ -106,6 +106,7 @@ def test_refusals_without_a_gpu():
     assert call(n=B.dynmo_grouped_ffn_mxfp4_workspace_bytes(d) - 1) == -3
     assert call(desc=B.make_desc(8, 16, 16, 4, 2, "f32")) == -2
     assert call(desc=B.make_desc(8, (1 << 22) + 8, 16, 4, 2, "bf16")) == -2
+    assert call(desc=B.make_desc(1 << 27, 8, 8, 4, 2, "bf16")) == -2  # 2^24 row blocks
     assert call(desc=B.make_desc(8, 16, 16, 65, 2, "bf16")) == -2 and call(desc=B.make_desc(8, 12, 16, 4, 2, "bf16")) == -2
     assert call(desc=B.make_desc(8, 16, 16, 4, 5, "bf16")) == -1
     assert B.dynmo_grouped_ffn_mxfp4_workspace_bytes(B.make_desc(8, 16, 16, 4, 2, "f32")) == 0

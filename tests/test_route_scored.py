@@ -91,7 +91,7 @@ def test_refusals_without_a_gpu():
     assert call(groups=4, top_groups=1, k=3) == -1             # a group has two experts
     assert call(group_best=0) == -1 and call(group_best=3) == -1
     assert call(scale=float("inf")) == -1 and call(scale=float("nan")) == -1
-    assert call(E=257) == -2 and call(k=9) == -1
+    assert call(E=257) == -2 and call(k=9) == -1 and call(T=1 << 26) == -2
     assert call(E=256, k=256, T=0) == 0 and call(E=64, k=8, T=0, groups=64, top_groups=8) == 0
     bad = B.make_rule()
     bad.score = 2
@@ -173,7 +173,7 @@ def check_bwd(lg, idx, k, rule, rng):
                              torch.from_numpy(idx).cuda(), out)
     how = dict(score=rule["score"], renormalize=rule["renormalize"], scale=rule["scale"])
     ref = orc.route_scored_bwd(dg, lg, idx, **how)
-    # the largest term: ds s, with ds up to |g| / S + |g| s / S^2, and s / S at most 1
+    # the largest term: w_j |g_j| and w_j sum |g_i| w_i (as they are: s instead of w)
     s, _ = orc.route_scores(lg, rule["score"])
     grad_size = 2 * np.abs(dg).sum(1) * abs(rule["scale"])
     if not rule["renormalize"]:
@@ -245,8 +245,10 @@ def test_scores_that_vanish_or_saturate(score, E, groups, top):
         bias = None if bias is None else (bias + 0.01 * rng.standard_normal(E)).astype(np.float32)
         for best in (1, 2):
             rule = dict(score=score, groups=groups, top_groups=top, group_best=best, renormalize=True, scale=1.0)
-            check_route(lg, bias, 3, rule)
+            idx = check_route(lg, bias, 3, rule)
+            check_bwd(lg, idx, 3, rule, rng)
             check_route(lg, bias, 3, dict(rule, renormalize=False))
+            check_bwd(lg, idx, 3, dict(rule, renormalize=False), rng)
 
 
 @pytest.mark.gpu
