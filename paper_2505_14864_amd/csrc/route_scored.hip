@@ -380,22 +380,27 @@ __global__ __launch_bounds__(256) void route_scored_kernel(const float* __restri
         v64[q] = mine ? -INFINITY : v64[q];
       }
     }
-    double total64 = 1.0;
-    if (rule.renormalize) {  // relative to the largest chosen score (of a sigmoid, to e^z of it where that is below one): they may all be tiny
+    auto chosen_sum = [&]() {
+      double sum = 0.0;
+#pragma unroll
+      for (int q = 0; q < VPL; ++q) sum += slot64[q] >= 0 ? s64[q] : 0.0;
+#pragma unroll
+      for (int n = 1; n < LPT; n <<= 1) sum += __shfl_xor(sum, n, 64);
+      return sum;
+    };
+    double total64 = rule.renormalize ? chosen_sum() : 1.0;
+    if (__ballot(total64 < 1e-290)) {  // scores that vanish: relative to the largest chosen one (of a sigmoid, to e^z of it where that is below one)
       float m = -INFINITY;
 #pragma unroll
       for (int q = 0; q < VPL; ++q) m = slot64[q] >= 0 ? fmaxf(m, z[q]) : m;
       m = max_over<LPT>(m);
       if (!softmax) m = fminf(m, 0.f);
-      total64 = 0.0;
 #pragma unroll
       for (int q = 0; q < VPL; ++q) {
         const double up = softmax || z[q] <= 0.f ? exp((double)z[q] - (double)m) : 1.0;
         s64[q] = slot64[q] >= 0 ? (softmax ? up : up / (1.0 + exp(-fabs((double)z[q])))) : 0.0;
-        total64 += s64[q];
       }
-#pragma unroll
-      for (int n = 1; n < LPT; n <<= 1) total64 += __shfl_xor(total64, n, 64);
+      total64 = chosen_sum();
     }
     if (sum_over<LPT>(doubtful ? 1.f : 0.f) > 0.f) {
       filled = filled64;
