@@ -12,9 +12,9 @@
 // scales of four steps come with every fourth.  A load has a descriptor that stays and a scalar offset that moves: with addresses worked
 // out per load the scalar instructions took 15 % (gate/up of 8192 rows 686 -> 600 us).
 //
-// Bound, 8192 rows over 8 experts, 4096 x 14336: gate/up 3.6 PFLOP/s, down 3.4, of 6.5 to 7 that the instruction alone reaches on random operands from
-// registers.  Both are held by the chip's power: the clock is at 1.76 GHz here, and the same launches on operands of zeros take 443 and 233
-// us instead of 590 and 291.  What is left at that is the loads (447 and 202 us without them, 355 and 234 without the matrix instructions and
+// Bound, 8192 rows over 8 experts, 4096 x 14336: gate/up 3.6 PFLOP/s (534 us), down 3.4 (284), of 6.5 to 7 that the instruction alone reaches on random operands from
+// registers.  Both are held by the chip's power: the clock is at 1.9 GHz here with the matrix pipes busy half of the time, and the same launches on
+// operands of zeros took 443 and 233 us when they took 590 and 291.  What is left at that is the loads (447 and 202 us without them, 355 and 234 without the matrix instructions and
 // the reads).  Measured and no faster: tiles of 256 x 256 by eight wavefronts (603, 324) or by four of 128 x 128 (667, 330), 128 x 256 (595, 293), the next
 // step's operands read from LDS during the present one (609, 304), row tiles walked in chunks of 8, 12 or 16.  Two stages instead of three: down of 256
 // rows 51 -> 83 us; four: a workgroup less per compute unit, gate/up of 64 ragged experts 67 -> 75, of 2000 rows 165 -> 215.

@@ -1,8 +1,6 @@
 // MXFP4 quantisation and its reverse.  Bound by memory: a value is read once and 17/32 byte written (or the other way round).
 #include "ffn_mxfp4.h"
 
-#include "profile.h"
-
 namespace dynmo {
 
 // A wavefront takes tiles of 16 rows x 128 values, one after another along a row block, and asks for the next one before it works on the

@@ -13,8 +13,9 @@
 // as many lanes as it needs, 4, 16 or 64, so that up to 16 tokens share a wavefront; a maximum over a token's lanes takes two, four or
 // eight vector instructions for all of them at once, and the winner's own lane stores its index and weight: nothing else crosses lanes.
 //
-// Measured: 65536 tokens x 64 experts, k = 8, with a bias 20 us (all of it in 64 bits, a token per wavefront: 101), 4096 x 256 in eight groups 14
-// (18; of these 14 the doubtful tokens are 4), 3001 x 60 in five groups 5 (9), one token 2.3; backward 65536 x 256 22 us, 3 TB/s of gradients written.
+// Measured: 65536 tokens x 64 experts, k = 8, with a bias 20 us, without one 15 (all of it in 64 bits, a token per wavefront: 101 with it),
+// 4096 x 256 in eight groups 8 to 12, by whether a token is in doubt (18), 3001 x 60 in five groups 4.6 (9), one token 2.1, 65536 x 256 in groups 92; backward
+// 65536 x 256 21 us, 3.2 TB/s of gradients written.
 #include "common.h"
 #include "profile.h"
 
