@@ -319,7 +319,8 @@ size_t dynmo_grouped_ffn_mxfp4_workspace_bytes(const dynmo_desc* d);
  * dynmo_grouped_ffn_fwd_gather (of any size).  Wg, Wu [E, dynmo_mxfp4_bytes(F, H)], Wd [E, dynmo_mxfp4_bytes(H, F)].
  * G_save, U_save [T*k,F]: both, or both NULL.  With them, and with the weights dequantised to bfloat16,
  * dynmo_grouped_ffn_bwd gives the gradient that passes the quantisations straight through.
- * A row with an infinity or a NaN gives a row of NaN, other rows do not depend on it.  The workspace holds the quantised X and A. */
+ * A row with an infinity or a NaN gives a row of NaN, other rows do not depend on it.  The workspace holds the quantised X and A:
+ * two calls that overlap in time need separate workspaces. */
 int32_t dynmo_grouped_ffn_mxfp4(const dynmo_desc* d, const void* x, const int32_t* src_slot, const int32_t* seg_offsets, const void* Wg,
                                 const void* Wu, const void* Wd, void* y_p, void* G_save, void* U_save, void* workspace,
                                 size_t workspace_bytes, void* stream);

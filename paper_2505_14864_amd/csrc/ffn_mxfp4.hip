@@ -12,7 +12,7 @@
 // scales of four steps come with every fourth.  A load has a descriptor that stays and a scalar offset that moves: with addresses worked
 // out per load the scalar instructions took 15 % (gate/up of 8192 rows 686 -> 600 us).
 //
-// Bound, 8192 rows over 8 experts, 4096 x 14336: gate/up 3.6 PFLOP/s (534 us), down 3.4 (284), of 6.5 to 7 that the instruction alone reaches on random operands from
+// Bound, 8192 rows over 8 experts, 4096 x 14336: gate/up 3.6 PFLOP/s (534 us), down 3.4 (282), of 6.5 to 7 that the instruction alone reaches on random operands from
 // registers.  Both are held by the chip's power: the clock is at 1.9 GHz here with the matrix pipes busy half of the time, and the same launches on
 // operands of zeros took 443 and 233 us when they took 590 and 291.  What is left at that is the loads (447 and 202 us without them, 355 and 234 without the matrix instructions and
 // the reads).  Measured and no faster: tiles of 256 x 256 by eight wavefronts (603, 324) or by four of 128 x 128 (667, 330), 128 x 256 (595, 293), the next
@@ -217,14 +217,20 @@ static int32_t launch_mx(MxProduct p, const dynmo_desc* d, KernelId id, hipStrea
   return DYNMO_OK;
 }
 
-// Tiles of 256 weight rows where they fill the chip four times over (two workgroups on each of 256 compute units), of 128 (three) else.
-// Both, us: 8 experts, 8192 rows, 4096 x 14336, gate/up (8064 tiles of 256) 602 / 636, down 316 / 313; 2000 rows, gate/up (2688) 163 / 168,
-// down (400) 116 / 112; 16 experts, 32768 rows, 4096 x 688, gate/up (1664) 130 / 127, down (4352) 146 / 153; 8 experts, 2048 rows,
-// 2048 x 4096, gate/up (768) 39 / 33.
+// Tiles of 256 weight rows where they fill the chip four times over (two workgroups on each of 256 compute units), of 128 (three) else.  A
+// larger tile moves a quarter less through LDS and has a longer prologue and epilogue, so it also wins where few of them have a long k to go, and
+// not where many have a short one.  Both, us (tiles of 256):
+//   gate/up  8192 rows, 8 experts, 4096 x 14336 (8064) 602 / 636; 12000, 32, 3968 x 2816 (2816) 172 / 185; 6000, 8, 4096 x 8192 (3456) 223 / 233; 32768, 64,
+//            2048 x 1024 (2560) 97 / 98; 16384, 16, 1024 x 4096 (4608) 115 / 113; but 16384, 8, 512 x 2048 (2176) 45 / 41, 32768, 16, 4096 x 688 (1664) 130 / 127
+//   down     32768, 64, 1024 -> 2048 (2560) 66 / 69; 12000, 32, 2816 -> 3968 (2048) 101 / 107
+//            long sums: 8192, 1, 8192 -> 2048 (576) 65 / 79; 4000, 4, 14336 -> 4096 (576) 121 / 143; 6000, 8, 8192 -> 2048 (432) 66 / 76; 6000, 8, 8192 -> 4096
+//            (936) 129 / 135; but 4096, 4, 4096 -> 4096 (576) 57 / 48, 16384, 16, 4096 -> 1024 (576) 55 / 50, 2000, 8, 14336 -> 4096 (400) 116 / 112
 template <bool GATEUP>
 static int32_t mx_tiles(const MxProduct& p, const dynmo_desc* d, KernelId id, hipStream_t st) {
   using Wide = MxShape<8, 4, 2, 2>;
-  if (mx_tile_count<GATEUP, Wide>(p, d) >= 4 * 512) return launch_mx<GATEUP, Wide>(p, d, id, st);
+  const int64_t tiles = mx_tile_count<GATEUP, Wide>(p, d);
+  const int steps = mx_k_blocks(p.K);
+  if (GATEUP ? tiles >= 4 * 512 && steps >= 8 : tiles >= 4 * 512 || (tiles >= 416 && steps >= 64)) return launch_mx<GATEUP, Wide>(p, d, id, st);
   return launch_mx<GATEUP, MxShape<4, 4, 2, 2>>(p, d, id, st);
 }
 

@@ -283,6 +283,15 @@ def test_ffn(T, H, F, E, k, counts, gather):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T,H,F,E,counts,save", [(10700, 1032, 8200, 2, [300, 37], False), (52480, 1032, 264, 3, [130, 0, 257], False),
+                                                  (16000, 1032, 2056, 2, [17, 200], True)])
+def test_ffn_wide_tiles(T, H, F, E, counts, save):
+    """Sizes that take tiles of 256 weight rows (chosen by the rows there may be; few are routed here): gate/up and a down product with a long
+    sum, down by the number of its tiles, gate/up alone with G and U saved."""
+    check_ffn(T, H, F, E, 1, counts, True, save=save)
+
+
+@pytest.mark.gpu
 def test_ffn_workspace_at_any_address_and_nothing_written_behind_it():
     T, H, F, E, k = 20, 264, 136, 3, 2
     rng = np.random.default_rng(5)
