@@ -317,13 +317,25 @@ size_t dynmo_grouped_ffn_mxfp4_workspace_bytes(const dynmo_desc* d);
  * (T*k / 128 + min(E, T*k)) * max(F, H) / 64 up to 2^23 (DYNMO_EUNSUPPORTED where that leaves too many tiles for a launch).
  * src_slot NULL: x is x_p [T*k,H], expert-sorted rows; else x [T,H] in token order, row p being x[src_slot[p] / k] as for
  * dynmo_grouped_ffn_fwd_gather (of any size).  Wg, Wu [E, dynmo_mxfp4_bytes(F, H)], Wd [E, dynmo_mxfp4_bytes(H, F)].
- * G_save, U_save [T*k,F]: both, or both NULL.  With them, and with the weights dequantised to bfloat16,
- * dynmo_grouped_ffn_bwd gives the gradient that passes the quantisations straight through.
+ * G_save, U_save [T*k,F]: both, or both NULL; dynmo_grouped_ffn_mxfp4_bwd takes them.
  * A row with an infinity or a NaN gives a row of NaN, other rows do not depend on it.  The workspace holds the quantised X and A:
  * two calls that overlap in time need separate workspaces. */
 int32_t dynmo_grouped_ffn_mxfp4(const dynmo_desc* d, const void* x, const int32_t* src_slot, const int32_t* seg_offsets, const void* Wg,
                                 const void* Wu, const void* Wd, void* y_p, void* G_save, void* U_save, void* workspace,
                                 size_t workspace_bytes, void* stream);
+
+size_t dynmo_grouped_ffn_mxfp4_bwd_workspace_bytes(const dynmo_desc* d);
+
+/* Backward of dynmo_grouped_ffn_mxfp4, passing its quantisations straight through (their derivative counts as one, saturated values
+ * included): dA = dY Wd; dG = dA U silu'(G); dU = dA silu(G); dX = dG Wg + dU Wu; dWd[e] = dY_e^T Q(A)_e; dWg[e] = dG_e^T Q(X)_e; dWu[e] = dU_e^T Q(X)_e.
+ * fwd_workspace: the forward call's, as that call on the same descriptor and segments left it (not a copy at another address): it holds Q(X) and Q(A).
+ * G_save, U_save: of that call.  Wg, Wu [E,F,H], Wd [E,H,F] in bfloat16, as dynmo_mxfp4_dequantize gives them.  Everything else as for
+ * dynmo_grouped_ffn_bwd, whose weight gradients after that forward call would be those of the X and silu(G) U that were not quantised.  DYNMO_BF16
+ * only, limits as for the forward call. */
+int32_t dynmo_grouped_ffn_mxfp4_bwd(const dynmo_desc* d, const void* dy_p, const void* fwd_workspace, size_t fwd_workspace_bytes,
+                                    const void* G_save, const void* U_save, const int32_t* seg_offsets, const void* Wg, const void* Wu,
+                                    const void* Wd, void* dx_p, void* dWg, void* dWu, void* dWd, void* workspace, size_t workspace_bytes,
+                                    void* stream);
 
 /* ---- combine ----------------------------------------------------------- */
 

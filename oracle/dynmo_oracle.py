@@ -417,6 +417,25 @@ def grouped_ffn_mxfp4(x_p, seg_offsets, Wg, Wu, Wd):
     return Y, G, U, A
 
 
+def grouped_ffn_mxfp4_bwd(dy_p, x_p, A, G, U, seg_offsets, Wg, Wu, Wd):
+    """Backward of grouped_ffn_mxfp4 with the quantisations' derivatives counted as one: of the functions Q(X) = X + c and Q(A) = A + c' with
+    c and c' constant.  A: before its quantisation, as the forward pass returns it.  Returns dx, dWg, dWu, dWd."""
+    Wg, Wu, Wd, dy_p = _f64(Wg), _f64(Wu), _f64(Wd), _f64(dy_p)
+    x_q, a_q = mxfp4_quantize(x_p)[0], mxfp4_quantize(A)[0]
+    s = _sigmoid(_f64(G))
+    silu, dsilu = _f64(G) * s, s + _f64(G) * s * (1.0 - s)
+    dx = np.zeros(x_q.shape, F64)
+    dWg, dWu, dWd = np.zeros_like(Wg), np.zeros_like(Wu), np.zeros_like(Wd)
+    for e in range(Wg.shape[0]):
+        rows = slice(int(seg_offsets[e]), int(seg_offsets[e + 1]))
+        dA = dy_p[rows] @ Wd[e]
+        dG, dU = dA * _f64(U)[rows] * dsilu[rows], dA * silu[rows]
+        dx[rows] = dG @ Wg[e] + dU @ Wu[e]
+        dWg[e], dWu[e] = dG.T @ x_q[rows], dU.T @ x_q[rows]
+        dWd[e] = dy_p[rows].T @ a_q[rows]
+    return dx, dWg, dWu, dWd
+
+
 def grouped_ffn_bwd(dy_p, x_p, G, U, seg_offsets, Wg, Wu, Wd):
     """Backward of grouped_ffn_fwd.
 

@@ -79,6 +79,8 @@ SIGNATURES = {
     "dynmo_mxfp4_dequantize": (_I, [_I, _I, _I, _I, _P, _P, _P]),
     "dynmo_grouped_ffn_mxfp4_workspace_bytes": (C.c_size_t, [_D]),
     "dynmo_grouped_ffn_mxfp4": (_I, [_D] + [_P] * 10 + [C.c_size_t, _P]),
+    "dynmo_grouped_ffn_mxfp4_bwd_workspace_bytes": (C.c_size_t, [_D]),
+    "dynmo_grouped_ffn_mxfp4_bwd": (_I, [_D] + [_P] * 2 + [C.c_size_t] + [_P] * 11 + [C.c_size_t, _P]),
     "dynmo_combine": (_I, [_D, _P, _P, _P, _P, _P, _P]),
     "dynmo_combine_bwd": (_I, [_D, _P, _P, _P, _P, _P, _P, _P]),
     "dynmo_layer_load": (_I, [_D, _P, C.c_double, C.POINTER(C.c_int32), C.POINTER(C.c_double), _P]),
@@ -218,6 +220,7 @@ for _name, _kinds in {
     "dynmo_grouped_ffn_fwd_gather": "dtttttttttws", "dynmo_grouped_ffn_fwd_combine": "dtttttttttttttws",
     "dynmo_grouped_ffn_bwd": "dttttttttttttws", "dynmo_grouped_ffn_bwd_scatter": "dtttttttttttttttws",
     "dynmo_mxfp4_quantize": "iiiitts", "dynmo_mxfp4_dequantize": "iiiitts", "dynmo_grouped_ffn_mxfp4": "dtttttttttws",
+    "dynmo_grouped_ffn_mxfp4_bwd": "dtwttttttttttws",
     "dynmo_combine": "dttttts", "dynmo_combine_bwd": "dtttttts",
 }.items():
     setattr(_launch, _name, _Launch(_name, _kinds))
@@ -381,6 +384,14 @@ def dynmo_grouped_ffn_mxfp4_workspace_bytes(d):
 
 def dynmo_grouped_ffn_mxfp4(d, x, src_slot, seg_offsets, Wg, Wu, Wd, y_p, G_save, U_save, workspace, stream=None):
     _launch.dynmo_grouped_ffn_mxfp4(d, x, src_slot, seg_offsets, Wg, Wu, Wd, y_p, G_save, U_save, workspace, stream)
+
+
+def dynmo_grouped_ffn_mxfp4_bwd_workspace_bytes(d):
+    return lib().dynmo_grouped_ffn_mxfp4_bwd_workspace_bytes(C.byref(d))
+
+
+def dynmo_grouped_ffn_mxfp4_bwd(d, dy_p, fwd_workspace, G_save, U_save, seg_offsets, Wg, Wu, Wd, dx_p, dWg, dWu, dWd, workspace, stream=None):
+    _launch.dynmo_grouped_ffn_mxfp4_bwd(d, dy_p, fwd_workspace, G_save, U_save, seg_offsets, Wg, Wu, Wd, dx_p, dWg, dWu, dWd, workspace, stream)
 
 
 def dynmo_combine(d, y_p, dst_pos, gate_w, base, out, stream=None):

@@ -36,6 +36,13 @@ struct FoldedCombine {
   void* out;
 };
 
+// Q(X) and Q(A) of a forward pass on MXFP4 weights, as its workspace holds them (mxfp4.h): codes and scales of the segments' row
+// blocks.  Backward unpacks them into `rows` [T*k, H], which x_p then is, and over the A that the dA product formed from G and U.
+struct MxSaved {
+  const void *x, *xs, *a, *as;
+  void* rows;
+};
+
 // In both forward families `gather` is NULL (x_p holds the expert-sorted rows) or the
 // slot index: row p is then x_p[gather[p] / k], x_p being the token-ordered input.
 // `fc` is NULL or the folded combine; y_p (forward) / dx_p (backward) may be NULL only with it.
@@ -54,9 +61,16 @@ size_t ffn_mfma_scratch_bytes();  // 256-byte aligned device scratch both calls 
 int32_t ffn_fwd_mfma(const dynmo_desc* d, const void* x_p, const int32_t* gather, const int32_t* seg, const void* Wg,
                      const void* Wu, const void* Wd, void* y_p, void* G, void* U, void* A, void* scratch,
                      const FoldedCombine* fc, hipStream_t st);
+// `mx`: NULL, or the rows and the A that the weight gradients are taken from in place of x_p and silu(G) U
 int32_t ffn_bwd_mfma(const dynmo_desc* d, const void* dy_p, const void* x_p, const void* G, const void* U,
                      const int32_t* seg, const void* Wg, const void* Wu, const void* Wd, void* dx_p, void* dWg,
                      void* dWu, void* dWd, void* dG, void* dU, void* A, void* scratch, const FoldedCombine* fc,
-                     hipStream_t st);
+                     const MxSaved* mx, hipStream_t st);
+
+// ffn.hip: the checks of the backward calls, and the choice of the family
+int32_t ffn_bwd_entry(const dynmo_desc* d, const void* dy_p, const void* x_p, const void* G_save, const void* U_save,
+                      const int32_t* seg_offsets, const void* Wg, const void* Wu, const void* Wd, void* dx_p, void* dWg,
+                      void* dWu, void* dWd, void* workspace, size_t workspace_bytes, const FoldedCombine* fc,
+                      const MxSaved* mx, void* stream);
 
 }  // namespace dynmo

@@ -89,10 +89,10 @@ extern "C" int32_t dynmo_grouped_ffn_fwd_combine(const dynmo_desc* d, const void
 }
 
 namespace dynmo {
-static int32_t ffn_bwd_entry(const dynmo_desc* d, const void* dy_p, const void* x_p, const void* G_save,
-                             const void* U_save, const int32_t* seg_offsets, const void* Wg, const void* Wu,
-                             const void* Wd, void* dx_p, void* dWg, void* dWu, void* dWd, void* workspace,
-                             size_t workspace_bytes, const FoldedCombine* fc, void* stream) {
+int32_t ffn_bwd_entry(const dynmo_desc* d, const void* dy_p, const void* x_p, const void* G_save, const void* U_save,
+                      const int32_t* seg_offsets, const void* Wg, const void* Wu, const void* Wd, void* dx_p, void* dWg,
+                      void* dWu, void* dWd, void* workspace, size_t workspace_bytes, const FoldedCombine* fc,
+                      const MxSaved* mx, void* stream) {
   int32_t rc = check_desc(d);
   if (rc) return rc;
   if (!dy_p || !x_p || !G_save || !U_save || !seg_offsets || !Wg || !Wu || !Wd || !dWg || !dWu || !dWd || !workspace)
@@ -107,7 +107,7 @@ static int32_t ffn_bwd_entry(const dynmo_desc* d, const void* dy_p, const void* 
   void* A = base + 2 * act_bytes(d);
   if (ffn_mfma_supported(d))
     return ffn_bwd_mfma(d, dy_p, x_p, G_save, U_save, seg_offsets, Wg, Wu, Wd, dx_p, dWg, dWu, dWd, dG, dU, A,
-                        base + 3 * act_bytes(d), fc, (hipStream_t)stream);
+                        base + 3 * act_bytes(d), fc, mx, (hipStream_t)stream);
   if (d->dtype != DYNMO_F32) return DYNMO_EUNSUPPORTED;       // more tiles than the bf16 kernels can count (70 TB of G)
   if (max_m_tiles(d, 64) > 65535) return DYNMO_EUNSUPPORTED;  // the fp32 kernels put row tiles on grid y
   return ffn_bwd_f32(d, dy_p, x_p, G_save, U_save, seg_offsets, Wg, Wu, Wd, dx_p, dWg, dWu, dWd, dG, dU, A, fc,
@@ -120,7 +120,7 @@ extern "C" int32_t dynmo_grouped_ffn_bwd(const dynmo_desc* d, const void* dy_p, 
                                          const void* Wu, const void* Wd, void* dx_p, void* dWg, void* dWu, void* dWd,
                                          void* workspace, size_t workspace_bytes, void* stream) {
   return ffn_bwd_entry(d, dy_p, x_p, G_save, U_save, seg_offsets, Wg, Wu, Wd, dx_p, dWg, dWu, dWd, workspace,
-                       workspace_bytes, nullptr, stream);
+                       workspace_bytes, nullptr, nullptr, stream);
 }
 
 extern "C" int32_t dynmo_grouped_ffn_bwd_scatter(const dynmo_desc* d, const void* dy_p, const void* x_p,
@@ -133,5 +133,5 @@ extern "C" int32_t dynmo_grouped_ffn_bwd_scatter(const dynmo_desc* d, const void
   if (d->k != 1) return DYNMO_EINVAL;  // with two slots per token two rows would meet in one row of dx
   const FoldedCombine fc = {src_slot, nullptr, dbase, dx};
   return ffn_bwd_entry(d, dy_p, x_p, G_save, U_save, seg_offsets, Wg, Wu, Wd, dx_p, dWg, dWu, dWd, workspace,
-                       workspace_bytes, &fc, stream);
+                       workspace_bytes, &fc, nullptr, stream);
 }

@@ -45,6 +45,7 @@
 #include <math.h>
 
 #include "ffn_gemm.h"
+#include "mxfp4.h"
 
 namespace dynmo {
 
@@ -1443,7 +1444,7 @@ int32_t ffn_fwd_mfma(const dynmo_desc* d, const void* x_p, const int32_t* gather
 int32_t ffn_bwd_mfma(const dynmo_desc* d, const void* dy_p, const void* x_p, const void* G, const void* U,
                      const int32_t* seg, const void* Wg, const void* Wu, const void* Wd, void* dx_p, void* dWg,
                      void* dWu, void* dWd, void* dG, void* dU, void* A, void* scratch, const FoldedCombine* fc,
-                     hipStream_t st) {
+                     const MxSaved* mx, hipStream_t st) {
   const long FH = (long)d->F * d->H;
   int32_t rc;
   {  // dA = dY Wd, epilogue -> A, dG, dU
@@ -1464,6 +1465,10 @@ int32_t ffn_bwd_mfma(const dynmo_desc* d, const void* dy_p, const void* x_p, con
     p.G = (const bf16_t*)G;
     p.U = (const bf16_t*)U;
     if ((rc = launch_rows_product<MODE_DA>(d, p, K_FFN_DA, st))) return rc;
+  }
+  if (mx) {
+    if ((rc = mx_dequantize_segments(d, mx->x, mx->xs, seg, d->H, (bf16_t*)mx->rows, st))) return rc;
+    if ((rc = mx_dequantize_segments(d, mx->a, mx->as, seg, d->F, (bf16_t*)A, st))) return rc;
   }
   // weight gradients: contraction over the rows of each expert
   auto dw = [&](const void* P, int M, const void* Q, int N, void* out, KernelId id) -> int32_t {

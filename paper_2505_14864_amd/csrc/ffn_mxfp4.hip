@@ -247,6 +247,7 @@ static MxWorkspace mx_workspace(const dynmo_desc* d) {
   w.bytes = w.as + blocks * mx_k_quads(d->F) * kMxScales + 256;
   return w;
 }
+static size_t mx_rows_bytes(const dynmo_desc* d) { return align_up((size_t)d->T * d->k * d->H * elem_bytes(d->dtype), 256); }
 
 }  // namespace dynmo
 
@@ -301,4 +302,25 @@ extern "C" int32_t dynmo_grouped_ffn_mxfp4(const dynmo_desc* d, const void* x, c
   const int max_experts = (int)(rows < d->E ? rows : d->E);
   if (d->T <= 64 && (int64_t)max_experts * ((d->H + 127) / 128) <= 256) return mx_few_rows(p, max_experts, K_FFN_DOWN, st);
   return mx_tiles<false>(p, d, K_FFN_DOWN, st);
+}
+
+extern "C" size_t dynmo_grouped_ffn_mxfp4_bwd_workspace_bytes(const dynmo_desc* d) {
+  if (check_desc(d) || d->dtype != DYNMO_BF16) return 0;
+  return mx_rows_bytes(d) + dynmo_grouped_ffn_bwd_workspace_bytes(d);  // Q(X), and what the bf16 products need
+}
+
+extern "C" int32_t dynmo_grouped_ffn_mxfp4_bwd(const dynmo_desc* d, const void* dy_p, const void* fwd_workspace, size_t fwd_workspace_bytes,
+                                               const void* G_save, const void* U_save, const int32_t* seg_offsets, const void* Wg,
+                                               const void* Wu, const void* Wd, void* dx_p, void* dWg, void* dWu, void* dWd,
+                                               void* workspace, size_t workspace_bytes, void* stream) {
+  const int32_t rc = check_desc(d);
+  if (rc) return rc;
+  if (d->dtype != DYNMO_BF16 || d->H > 1 << 22 || d->F > 1 << 22 || mx_max_row_blocks(d) >= kMaxBlocks) return DYNMO_EUNSUPPORTED;
+  if (!fwd_workspace || !workspace) return DYNMO_EINVAL;
+  const MxWorkspace w = mx_workspace(d);
+  if (fwd_workspace_bytes < w.bytes || workspace_bytes < dynmo_grouped_ffn_mxfp4_bwd_workspace_bytes(d)) return DYNMO_EWORKSPACE;
+  const char* saved = (const char*)align_up((size_t)fwd_workspace, 256);
+  const MxSaved mx = {saved + w.x, saved + w.xs, saved + w.a, saved + w.as, (void*)align_up((size_t)workspace, 256)};
+  return ffn_bwd_entry(d, dy_p, mx.rows, G_save, U_save, seg_offsets, Wg, Wu, Wd, dx_p, dWg, dWu, dWd, (char*)workspace + mx_rows_bytes(d),
+                       workspace_bytes - mx_rows_bytes(d), nullptr, &mx, stream);
 }

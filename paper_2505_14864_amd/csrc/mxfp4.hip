@@ -110,20 +110,15 @@ __global__ __launch_bounds__(kQuantThreads) void mx_quantize_kernel(const T* __r
                    matrix + mx_code_bytes(Rb, K) + (size_t)rb * Kq * kMxScales);
 }
 
-// Values four at a time: a store of the wavefront covers the 128 values of two rows (fp32: 512 contiguous bytes each).  The stores
-// go past the caches (figures at load8); of 1003 x 1032 bf16 values 4.2 us either way.
-template <typename T>
-__global__ __launch_bounds__(kQuantThreads) void mx_dequantize_kernel(const char* __restrict__ packed, T* __restrict__ dst, int rows, int K) {
-  const int Kb = mx_k_blocks(K), Kq = mx_k_quads(K), Rb = mx_row_blocks(rows);
-  const unsigned kq = blockIdx.x % Kq, at = blockIdx.x / Kq;
-  const int rb = at % Rb;
-  const long m = at / Rb;
-  const char* matrix = packed + m * mx_bytes(rows, K);
-  const int lane = threadIdx.x & 63, tile = threadIdx.x >> 6, kb = kq * 4 + tile;
-  const int c0 = (lane & 31) * 4, k = kb * 128 + c0, g = c0 / 32;
+// A wavefront takes a tile, values four at a time: a store of the wavefront covers the 128 values of two rows (fp32: 512 contiguous bytes each).
+// `codes`, `scales`: of the row block; row(r): where row r of the sixteen goes, or nullptr behind the last one.  ONCE: the stores go past the caches
+// (figures at load8); of 1003 x 1032 bf16 values 4.2 us either way.
+template <bool ONCE, typename T, typename Row>
+__device__ __forceinline__ void dequantize_tile(const char* codes, const char* scales, int kb, int K, Row&& row) {
+  const int lane = threadIdx.x & 63, c0 = (lane & 31) * 4, k = kb * 128 + c0, g = c0 / 32;
   if (k >= K) return;
-  const char* codes = matrix + ((size_t)rb * Kb + kb) * kMxTile + g * 256 + c0 % 32 / 2;
-  const char* scales = matrix + mx_code_bytes(Rb, K) + ((size_t)rb * Kq + kq) * kMxScales + g * 64 + tile;
+  codes += (size_t)kb * kMxTile + g * 256 + c0 % 32 / 2;
+  scales += (size_t)(kb / 4) * kMxScales + g * 64 + kb % 4;
   uint32_t code[8], byte[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {  // behind the last row there are zeros
@@ -132,16 +127,47 @@ __global__ __launch_bounds__(kQuantThreads) void mx_dequantize_kernel(const char
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int r = rb * 16 + 2 * i + (lane >> 5);
-    if (r >= rows) break;
+    T* to = row(2 * i + (lane >> 5));
+    if (!to) break;
+    to += k;
     const float scale = mx_scale_value(byte[i]);
     f32x2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[i], scale, 0), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[i], scale, 1);
     if (byte[i] == 255) lo.x = lo.y = hi.x = hi.y = __uint_as_float(0x7fc00000u);
-    T* to = dst + (m * rows + r) * (long)K + k;
     typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-    if constexpr (sizeof(T) == 2) __builtin_nontemporal_store(u32x2{pack_bf16x2(lo.x, lo.y), pack_bf16x2(hi.x, hi.y)}, (u32x2*)to);
-    else __builtin_nontemporal_store(u32x4{__float_as_uint(lo.x), __float_as_uint(lo.y), __float_as_uint(hi.x), __float_as_uint(hi.y)}, (u32x4*)to);
+    auto store = [](auto v, auto* p) {
+      if constexpr (ONCE) __builtin_nontemporal_store(v, p);
+      else *p = v;
+    };
+    if constexpr (sizeof(T) == 2) store(u32x2{pack_bf16x2(lo.x, lo.y), pack_bf16x2(hi.x, hi.y)}, (u32x2*)to);
+    else store(u32x4{__float_as_uint(lo.x), __float_as_uint(lo.y), __float_as_uint(hi.x), __float_as_uint(hi.y)}, (u32x4*)to);
   }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kQuantThreads) void mx_dequantize_kernel(const char* __restrict__ packed, T* __restrict__ dst, int rows, int K) {
+  const int Kb = mx_k_blocks(K), Kq = mx_k_quads(K), Rb = mx_row_blocks(rows);
+  const unsigned kq = blockIdx.x % Kq, at = blockIdx.x / Kq;
+  const int rb = at % Rb;
+  const long m = at / Rb;
+  const char* matrix = packed + m * mx_bytes(rows, K);
+  dequantize_tile<true, T>(matrix + (size_t)rb * Kb * kMxTile, matrix + mx_code_bytes(Rb, K) + (size_t)rb * Kq * kMxScales,
+                           kq * 4 + (threadIdx.x >> 6), K, [&](int r) -> T* {
+                             return rb * 16 + r < rows ? dst + (m * rows + rb * 16 + r) * (long)K : nullptr;
+                           });
+}
+
+// Row block rb of the segments: its rows are first .. last - 1, up to sixteen of them counted from first.  false: there is no such block.
+__device__ __forceinline__ bool segment_block(const int32_t* __restrict__ seg, int E, int rb, int* first, int* last) {
+  // lane e counts the row blocks of expert e; a prefix sum and a ballot find the owner of block rb
+  const int lane = threadIdx.x & 63;
+  const int begin = lane < E ? seg[lane] : 0, end = lane < E ? seg[lane + 1] : 0;
+  const int blocks = mx_row_blocks(end - begin), upto = experts_upto(blocks);
+  const unsigned long long owners = __ballot(upto > rb);
+  if (owners == 0) return false;
+  const int e = __builtin_ctzll(owners);
+  *first = __builtin_amdgcn_readlane(begin, e) + (rb - (__builtin_amdgcn_readlane(upto, e) - __builtin_amdgcn_readlane(blocks, e))) * 16;
+  *last = __builtin_amdgcn_readlane(end, e);
+  return true;
 }
 
 template <typename T>
@@ -149,16 +175,9 @@ __global__ __launch_bounds__(kQuantThreads) void mx_quantize_segments_kernel(con
                                                                              int gather_div, const int32_t* __restrict__ seg, int E, int K, int parts,
                                                                              char* __restrict__ codes, char* __restrict__ scales) {
   const int Kb = mx_k_blocks(K), Kq = mx_k_quads(K);
-  const int part = blockIdx.x % (unsigned)parts, rb = blockIdx.x / (unsigned)parts;
-  // lane e counts the row blocks of expert e; a prefix sum and a ballot find the owner of block rb
-  const int lane = threadIdx.x & 63;
-  const int begin = lane < E ? seg[lane] : 0, end = lane < E ? seg[lane + 1] : 0;
-  const int blocks = mx_row_blocks(end - begin), upto = experts_upto(blocks);
-  const unsigned long long owners = __ballot(upto > rb);
-  if (owners == 0) return;
-  const int e = __builtin_ctzll(owners);
-  const int first = __builtin_amdgcn_readlane(begin, e) + (rb - (__builtin_amdgcn_readlane(upto, e) - __builtin_amdgcn_readlane(blocks, e))) * 16;
-  const int last = __builtin_amdgcn_readlane(end, e);
+  const int part = blockIdx.x % (unsigned)parts, rb = blockIdx.x / (unsigned)parts, lane = threadIdx.x & 63;
+  int first, last;
+  if (!segment_block(seg, E, rb, &first, &last)) return;
   const T* row[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -169,7 +188,18 @@ __global__ __launch_bounds__(kQuantThreads) void mx_quantize_segments_kernel(con
                    scales + (size_t)rb * Kq * kMxScales);
 }
 
-constexpr int64_t kMaxBlocks = 1 << 24;  // of 256 threads: a launch has fewer than 2^32
+template <typename T>
+__global__ __launch_bounds__(kQuantThreads) void mx_dequantize_segments_kernel(const char* __restrict__ codes, const char* __restrict__ scales,
+                                                                               const int32_t* __restrict__ seg, int E, int K, int parts,
+                                                                               T* __restrict__ dst) {
+  const int Kb = mx_k_blocks(K), Kq = mx_k_quads(K);
+  const int part = blockIdx.x % (unsigned)parts, rb = blockIdx.x / (unsigned)parts;
+  int first, last;
+  if (!segment_block(seg, E, rb, &first, &last)) return;
+  for (int kq = part; kq < Kq; kq += parts)
+    dequantize_tile<false, T>(codes + (size_t)rb * Kb * kMxTile, scales + (size_t)rb * Kq * kMxScales, kq * 4 + (threadIdx.x >> 6), K,
+                              [&](int r) -> T* { return first + r < last ? dst + (size_t)(first + r) * K : nullptr; });
+}
 
 // Workgroups per row block: as many as the block has tiles for, but no more than some eight per compute unit in all.
 static int parts_of(int64_t row_blocks, int K) {
@@ -185,6 +215,16 @@ int32_t mx_quantize_segments(const dynmo_desc* d, const void* x, const int32_t* 
   const int parts = parts_of(row_blocks, K);
   DYNMO_TIMED_LAUNCH(K_MXFP4_QUANTIZE, st, mx_quantize_segments_kernel<bf16_t><<<dim3((unsigned)(row_blocks * parts)), dim3(kQuantThreads), 0, st>>>(
                                                (const bf16_t*)x, gather, d->k, seg, d->E, K, parts, (char*)codes, (char*)scales));
+  return DYNMO_OK;
+}
+
+int32_t mx_dequantize_segments(const dynmo_desc* d, const void* codes, const void* scales, const int32_t* seg, int K, bf16_t* dst, hipStream_t st) {
+  const int64_t row_blocks = mx_max_row_blocks(d);
+  if (row_blocks == 0) return DYNMO_OK;
+  if (row_blocks >= kMaxBlocks) return DYNMO_EUNSUPPORTED;
+  const int parts = parts_of(row_blocks, K);
+  DYNMO_TIMED_LAUNCH(K_MXFP4_DEQUANTIZE, st, mx_dequantize_segments_kernel<bf16_t><<<dim3((unsigned)(row_blocks * parts)), dim3(kQuantThreads), 0, st>>>(
+                                                 (const char*)codes, (const char*)scales, seg, d->E, K, parts, dst));
   return DYNMO_OK;
 }
 

@@ -5,7 +5,7 @@ Holds the device buffers of one layer and issues the library calls in order:
             (or permute indices only -> grouped_ffn_fwd_gather -> combine,
              or, for k = 1, permute -> grouped_ffn_fwd_combine,
             or, with experts in 4 bits, permute -> grouped_ffn_mxfp4 -> combine)
-  backward: combine_bwd -> grouped_ffn_bwd -> permute_bwd -> route_bwd
+  backward: combine_bwd -> grouped_ffn_bwd (grouped_ffn_mxfp4_bwd) -> permute_bwd -> route_bwd
 Buffers come from torch (device memory only); every step is a library kernel.
 """
 from __future__ import annotations
@@ -35,7 +35,9 @@ def to_host(t: torch.Tensor) -> np.ndarray:
 
 
 class RoutedFFNLayer:
-    """Buffers and call order for one layer.  mode: "moe" | "mod" | "early_exit"."""
+    """Buffers and call order for one layer.  mode: "moe" | "mod" | "early_exit".
+
+    backward() is that of the forward method called last, on what it left in the buffers."""
 
     def __init__(self, T, H, F, E=1, k=1, dtype="bf16", mode="moe", device="cuda"):
         self.T, self.H, self.F, self.E, self.k = T, H, F, E, k
@@ -67,6 +69,8 @@ class RoutedFFNLayer:
         self._bwd_ready = False
         self._rule = None  # of the last route_scored, for route_bwd
         self._ws_mxfp4 = None
+        self._ws_mxfp4_bwd = None
+        self._last = "forward"  # what the last forward method left for a backward pass: "forward", "mxfp4", or None
         self._dev = dev
 
     def alloc_backward(self):
@@ -109,6 +113,7 @@ class RoutedFFNLayer:
     def forward(self, x, Wg, Wu, Wd, out=None):
         d = self.d
         out = self.out if out is None else out
+        self._last = "forward"
         B.dynmo_permute(d, x, self.expert_idx, self.x_p, self.seg_offsets, self.src_slot, self.dst_pos, self.ws_permute)
         B.dynmo_grouped_ffn_fwd(d, self.x_p, self.seg_offsets, Wg, Wu, Wd, self.y_p, self.G, self.U, self.ws_fwd)
         B.dynmo_combine(d, self.y_p, self.dst_pos, self.gate_w, x if self.residual else None, out)
@@ -119,6 +124,7 @@ class RoutedFFNLayer:
         src_slot (x_p is not written, so backward() cannot follow this call)."""
         d = self.d
         out = self.out if out is None else out
+        self._last = "forward"
         B.dynmo_permute(d, None, self.expert_idx, None, self.seg_offsets, self.src_slot, self.dst_pos, self.ws_permute)
         B.dynmo_grouped_ffn_fwd_gather(d, x, self.src_slot, self.seg_offsets, Wg, Wu, Wd, self.y_p, self.G, self.U,
                                        self.ws_fwd)
@@ -127,10 +133,11 @@ class RoutedFFNLayer:
 
     def forward_mxfp4(self, x, Wg, Wu, Wd, out=None, train=False):
         """Forward on weights in 4 bits (packed by binding.dynmo_mxfp4_quantize, [E, bytes] each); bf16 layers.  Without `train` the rows are read
-        from x through src_slot and nothing is kept; with it x_p, G and U are, and backward() may follow with the weights
-        dequantised to bf16 (the gradient passes the quantisations straight through)."""
+        from x through src_slot and nothing is kept: backward() refuses to follow.  With it x_p, G, U and the quantised rows and activations are, and
+        backward() may follow with the weights dequantised to bf16: all four gradients pass the quantisations straight through."""
         d = self.d
         out = self.out if out is None else out
+        self._last = "mxfp4" if train else None
         if self._ws_mxfp4 is None:
             self._ws_mxfp4 = torch.empty((B.dynmo_grouped_ffn_mxfp4_workspace_bytes(d),), dtype=torch.uint8, device=self._dev)
         B.dynmo_permute(d, x if train else None, self.expert_idx, self.x_p if train else None, self.seg_offsets, self.src_slot, self.dst_pos,
@@ -150,18 +157,27 @@ class RoutedFFNLayer:
         d = self.d
         if out is None:
             out = x if self.residual else self.out
+        self._last = "forward"
         B.dynmo_permute(d, x, self.expert_idx, self.x_p, self.seg_offsets, self.src_slot, self.dst_pos, self.ws_permute)
         B.dynmo_grouped_ffn_fwd_combine(d, self.x_p, None, self.src_slot, self.seg_offsets, Wg, Wu, Wd, self.gate_w,
                                         x if self.residual else None, out, self.y_p, self.G, self.U, self.ws_fwd)
         return out
 
     def backward(self, dout, Wg, Wu, Wd, dx=None):
+        if self._last is None:
+            raise ValueError("forward_mxfp4 without `train` keeps nothing for a backward pass")
         self.alloc_backward()
         d = self.d
         dx = self.dx if dx is None else dx
         B.dynmo_combine_bwd(d, dout, self.y_p, self.dst_pos, self.gate_w, self.dy_p, self.dgate)
-        B.dynmo_grouped_ffn_bwd(d, self.dy_p, self.x_p, self.G, self.U, self.seg_offsets, Wg, Wu, Wd, self.dx_p,
-                                self.dWg, self.dWu, self.dWd, self.ws_bwd)
+        if self._last == "mxfp4":
+            if self._ws_mxfp4_bwd is None:
+                self._ws_mxfp4_bwd = torch.empty((B.dynmo_grouped_ffn_mxfp4_bwd_workspace_bytes(d),), dtype=torch.uint8, device=self._dev)
+            B.dynmo_grouped_ffn_mxfp4_bwd(d, self.dy_p, self._ws_mxfp4, self.G, self.U, self.seg_offsets, Wg, Wu, Wd, self.dx_p,
+                                          self.dWg, self.dWu, self.dWd, self._ws_mxfp4_bwd)
+        else:
+            B.dynmo_grouped_ffn_bwd(d, self.dy_p, self.x_p, self.G, self.U, self.seg_offsets, Wg, Wu, Wd, self.dx_p,
+                                    self.dWg, self.dWu, self.dWd, self.ws_bwd)
         B.dynmo_permute_bwd(d, self.dx_p, self.dst_pos, dout if self.residual else None, dx)
         return dx
 
@@ -170,7 +186,9 @@ class RoutedFFNLayer:
         A layer with a residual ("mod", "early_exit") updates dout in place and returns it (the
         gradient of a token without a routed row passes through untouched); with `dx` given it
         writes the routed tokens' rows of `dx` instead (dbase = dout) and the other rows of
-        `dx` are the caller's.  A top-1 "moe" layer writes self.dx (every token has a row)."""
+        `dx` are the caller's.  A top-1 "moe" layer writes self.dx (every token has a row).  Not behind forward_mxfp4."""
+        if self._last != "forward":
+            raise ValueError("backward_folded does not follow forward_mxfp4")
         self.alloc_backward()
         d = self.d
         if dx is None:
