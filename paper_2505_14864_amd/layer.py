@@ -68,6 +68,7 @@ class RoutedFFNLayer:
         self._seg_event = torch.cuda.Event()
         self._bwd_ready = False
         self._rule = None  # of the last route_scored, for route_bwd
+        self._droute_scored = None  # what route_bwd then fills: droute, or [T, E] where that has T elements only
         self._ws_mxfp4 = None
         self._ws_mxfp4_bwd = None
         self._last = "forward"  # what the last forward method left for a backward pass: "forward", "mxfp4", or None
@@ -203,8 +204,12 @@ class RoutedFFNLayer:
         """`scores`: what the routing read, where its backward pass needs it (the logits of route_scored, the scores of route_capacity)."""
         self.alloc_backward()
         if self._rule is not None:
-            B.dynmo_route_scored_bwd(self.d, self._rule, self.dgate, scores, self.expert_idx, self.droute)
-        elif self.mode == "moe":
+            if self._droute_scored is None:
+                fits = self.droute.numel() == self.T * self.E
+                self._droute_scored = self.droute if fits else torch.empty((self.T, self.E), dtype=torch.float32, device=self._dev)
+            B.dynmo_route_scored_bwd(self.d, self._rule, self.dgate, scores, self.expert_idx, self._droute_scored)
+            return self._droute_scored
+        if self.mode == "moe":
             B.dynmo_route_topk_bwd(self.d, self.dgate, self.gate_w, self.expert_idx, self.droute)
         elif self.mode == "mod":
             B.dynmo_route_capacity_bwd(self.d, self.dgate, scores, self.expert_idx, self.droute)

@@ -1,0 +1,52 @@
+"""The layer's routing methods and the gradient that follows them: which call it is, and that its result fits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import dynmo_oracle as orc
+from paper_2505_14864_amd import binding as B
+from paper_2505_14864_amd.layer import RoutedFFNLayer
+
+
+def host_layer(monkeypatch, T, E, k, mode):
+    """A layer without a GPU: torch's pinned memory and events stand aside, and nothing may be launched."""
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, pin_memory=False, **kw: empty(*a, **kw))
+    monkeypatch.setattr(torch.cuda, "Event", lambda: None)
+    return RoutedFFNLayer(T, 16, 16, E, k, "bf16", mode, device="cpu")
+
+
+@pytest.mark.parametrize("mode", ["moe", "mod", "early_exit"])
+@pytest.mark.parametrize("E", [1, 4])
+@pytest.mark.parametrize("allocated", [False, True])
+def test_scored_gradient_has_room_for_every_logit(monkeypatch, mode, E, allocated):
+    T = 6
+    layer, seen = host_layer(monkeypatch, T, E, 1, mode), []
+    monkeypatch.setattr(B, "dynmo_route_scored", lambda *a, **kw: None)
+    monkeypatch.setattr(B, "dynmo_route_scored_bwd", lambda d, rule, dgate, logits, expert_idx, dlogits: seen.append(dlogits))
+    if allocated:
+        layer.alloc_backward()
+    logits = torch.zeros((T, E), dtype=torch.float32)
+    layer.route_scored(logits, B.make_rule())
+    got = layer.route_bwd(logits)
+    assert seen[0] is got and got.numel() == T * E
+    assert layer.droute.shape == ((T, E) if mode == "moe" else (T,))  # the other routings' stays as it is
+    assert (got is layer.droute) == (mode == "moe" or E == 1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mode", ["moe", "mod", "early_exit"])
+def test_scored_routing_of_a_layer_with_a_residual(mode):
+    T, E, k = 70, 5, 2
+    rng = np.random.default_rng(4)
+    lg, dg = rng.standard_normal((T, E)).astype(np.float32), rng.standard_normal((T, k)).astype(np.float32)
+    layer = RoutedFFNLayer(T, 16, 16, E, k, "bf16", mode)
+    layer.alloc_backward()
+    logits = torch.from_numpy(lg).cuda()
+    for score, renormalize in (("sigmoid", True), ("softmax", False)):
+        layer.route_scored(logits, B.make_rule(score, renormalize=renormalize))
+        layer.dgate.copy_(torch.from_numpy(dg))
+        idx, _ = orc.route_scored(lg, None, k, score, renormalize=renormalize)
+        assert np.array_equal(layer.expert_idx.cpu().numpy(), idx)
+        ref = orc.route_scored_bwd(dg, lg, idx, score, renormalize)
+        assert np.abs(layer.route_bwd(logits).cpu().numpy() - ref).max() <= 64 * 2.0 ** -24 * 2 * np.abs(dg).sum(1).max()
