@@ -34,10 +34,14 @@ def to_host(t: torch.Tensor) -> np.ndarray:
     return t.numpy()
 
 
+_OF_LAST = object()  # route_bwd: the rule of the routing method called last
+
+
 class RoutedFFNLayer:
     """Buffers and call order for one layer.  mode: "moe" | "mod" | "early_exit".
 
-    backward() is that of the forward method called last, on what it left in the buffers."""
+    backward() is that of the forward method called last, on what it left in the buffers, and route_bwd() that of the routing method called
+    last; a program that fills the buffers with calls of the binding says there which routing it was."""
 
     def __init__(self, T, H, F, E=1, k=1, dtype="bf16", mode="moe", device="cuda"):
         self.T, self.H, self.F, self.E, self.k = T, H, F, E, k
@@ -200,14 +204,17 @@ class RoutedFFNLayer:
                                         self.ws_bwd)
         return dx
 
-    def route_bwd(self, scores=None):
-        """`scores`: what the routing read, where its backward pass needs it (the logits of route_scored, the scores of route_capacity)."""
+    def route_bwd(self, scores=None, rule=_OF_LAST):
+        """`scores`: what the routing read, where its backward pass needs it (the logits of route_scored, the scores of route_capacity).
+        `rule`: for indices and weights that a call of the binding wrote into the layer's buffers: the rule of dynmo_route_scored, or None for
+        the routing of the layer's mode (dynmo_route_topk, dynmo_route_capacity).  Without it, of the routing method called last."""
         self.alloc_backward()
-        if self._rule is not None:
+        rule = self._rule if rule is _OF_LAST else rule
+        if rule is not None:
             if self._droute_scored is None:
                 fits = self.droute.numel() == self.T * self.E
                 self._droute_scored = self.droute if fits else torch.empty((self.T, self.E), dtype=torch.float32, device=self._dev)
-            B.dynmo_route_scored_bwd(self.d, self._rule, self.dgate, scores, self.expert_idx, self._droute_scored)
+            B.dynmo_route_scored_bwd(self.d, rule, self.dgate, scores, self.expert_idx, self._droute_scored)
             return self._droute_scored
         if self.mode == "moe":
             B.dynmo_route_topk_bwd(self.d, self.dgate, self.gate_w, self.expert_idx, self.droute)

@@ -34,6 +34,45 @@ def test_scored_gradient_has_room_for_every_logit(monkeypatch, mode, E, allocate
     assert (got is layer.droute) == (mode == "moe" or E == 1)
 
 
+def test_the_gradient_is_that_of_the_last_routing(monkeypatch):
+    layer, seen = host_layer(monkeypatch, 6, 4, 2, "moe"), []
+    for name in ("dynmo_route_topk", "dynmo_route_scored", "dynmo_route_topk_bwd"):
+        monkeypatch.setattr(B, name, lambda *a, name=name, **kw: seen.append(name))
+    monkeypatch.setattr(B, "dynmo_route_scored_bwd", lambda d, rule, *a, **kw: seen.append(rule))
+    logits, rule, other = torch.zeros((6, 4), dtype=torch.float32), B.make_rule(), B.make_rule("sigmoid")
+
+    def gradient_of(*args, **kw):
+        seen.clear()
+        layer.route_bwd(*args, **kw)
+        return seen[0]
+
+    layer.route_scored(logits, rule)
+    assert gradient_of(logits) is rule
+    # calls of the binding into the layer's buffers: the caller says which
+    assert gradient_of(rule=None) == "dynmo_route_topk_bwd"
+    assert gradient_of(logits, rule=other) is other
+    assert gradient_of(logits) is rule
+    layer.route_topk(logits)
+    assert gradient_of() == "dynmo_route_topk_bwd"
+    assert gradient_of(logits, rule=other) is other
+
+
+@pytest.mark.gpu
+def test_gradient_of_a_binding_call_behind_a_scored_routing():
+    T, E, k = 40, 6, 2
+    rng = np.random.default_rng(5)
+    lg, dg = rng.standard_normal((T, E)).astype(np.float32), rng.standard_normal((T, k)).astype(np.float32)
+    layer = RoutedFFNLayer(T, 16, 16, E, k, "bf16")
+    layer.alloc_backward()
+    logits = torch.from_numpy(lg).cuda()
+    layer.route_scored(logits, B.make_rule("sigmoid", scale=3.0))
+    B.dynmo_route_topk(layer.d, logits, layer.expert_idx, layer.gate_w)
+    layer.dgate.copy_(torch.from_numpy(dg))
+    idx, gate = orc.route_topk(lg, k)
+    ref = orc.route_scored_bwd(dg, lg, idx, "softmax")  # the softmax over the chosen logits is the renormalised one
+    assert np.abs(layer.route_bwd(rule=None).cpu().numpy() - ref).max() <= 64 * 2.0 ** -24 * 2 * np.abs(dg).sum(1).max()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("mode", ["moe", "mod", "early_exit"])
 def test_scored_routing_of_a_layer_with_a_residual(mode):
