@@ -200,18 +200,20 @@ __global__ __launch_bounds__(S::kThreads, 2) void ffn_mx_kernel(const MxProduct 
   }
 }
 
+// The most output tiles that a product can have
 template <bool GATEUP, class S>
-static int64_t mx_tile_count(const MxProduct& p, const dynmo_desc* d) {
+static int64_t mx_tile_count(const dynmo_desc* d) {
   constexpr int TN = S::kWBlocks * 16 / (GATEUP ? 2 : 1), TM = S::kTBlocks * 16;
   const int64_t rows = (int64_t)d->T * d->k, row_tiles = rows / TM + (rows < d->E ? rows : d->E);
-  return row_tiles * (((GATEUP ? (int64_t)mx_k_blocks(p.N) * 128 : p.N) + TN - 1) / TN);
+  return row_tiles * (((GATEUP ? (int64_t)mx_k_blocks(d->F) * 128 : d->H) + TN - 1) / TN);
 }
+// A launch has fewer than 2^32 threads; the list is rounded up to whole runs
+constexpr int64_t kMaxTiles = (1 << 24) - (1 << 12);
 
 template <bool GATEUP, class S>
 static int32_t launch_mx(MxProduct p, const dynmo_desc* d, KernelId id, hipStream_t st) {
-  const int64_t tiles = mx_tile_count<GATEUP, S>(p, d);
+  const int64_t tiles = mx_tile_count<GATEUP, S>(d);
   if (tiles == 0) return DYNMO_OK;
-  if (tiles > (1 << 24) - (1 << 12)) return DYNMO_EUNSUPPORTED;  // a launch has fewer than 2^32 threads; the list is rounded up to whole runs
   p.list = tile_list((int)tiles);
   DYNMO_TIMED_LAUNCH(id, st, ffn_mx_kernel<GATEUP, S><<<dim3(p.list.blocks), dim3(S::kThreads), 0, st>>>(p));
   return DYNMO_OK;
@@ -225,13 +227,32 @@ static int32_t launch_mx(MxProduct p, const dynmo_desc* d, KernelId id, hipStrea
 //   down     32768, 64, 1024 -> 2048 (2560) 66 / 69; 12000, 32, 2816 -> 3968 (2048) 101 / 107
 //            long sums: 8192, 1, 8192 -> 2048 (576) 65 / 79; 4000, 4, 14336 -> 4096 (576) 121 / 143; 6000, 8, 8192 -> 2048 (432) 66 / 76; 6000, 8, 8192 -> 4096
 //            (936) 129 / 135; but 4096, 4, 4096 -> 4096 (576) 57 / 48, 16384, 16, 4096 -> 1024 (576) 55 / 50, 2000, 8, 14336 -> 4096 (400) 116 / 112
+using Wide = MxShape<8, 4, 2, 2>;
+using Narrow = MxShape<4, 4, 2, 2>;
+template <bool GATEUP>
+static bool takes_wide(const dynmo_desc* d) {
+  const int64_t tiles = mx_tile_count<GATEUP, Wide>(d);
+  const int steps = mx_k_blocks(GATEUP ? d->H : d->F);
+  return GATEUP ? tiles >= 4 * 512 && steps >= 8 : tiles >= 4 * 512 || (tiles >= 416 && steps >= 64);
+}
 template <bool GATEUP>
 static int32_t mx_tiles(const MxProduct& p, const dynmo_desc* d, KernelId id, hipStream_t st) {
-  using Wide = MxShape<8, 4, 2, 2>;
-  const int64_t tiles = mx_tile_count<GATEUP, Wide>(p, d);
-  const int steps = mx_k_blocks(p.K);
-  if (GATEUP ? tiles >= 4 * 512 && steps >= 8 : tiles >= 4 * 512 || (tiles >= 416 && steps >= 64)) return launch_mx<GATEUP, Wide>(p, d, id, st);
-  return launch_mx<GATEUP, MxShape<4, 4, 2, 2>>(p, d, id, st);
+  return takes_wide<GATEUP>(d) ? launch_mx<GATEUP, Wide>(p, d, id, st) : launch_mx<GATEUP, Narrow>(p, d, id, st);
+}
+template <bool GATEUP>
+static bool too_many_tiles(const dynmo_desc* d) {
+  return (takes_wide<GATEUP>(d) ? mx_tile_count<GATEUP, Wide>(d) : mx_tile_count<GATEUP, Narrow>(d)) > kMaxTiles;
+}
+// Up to 64 tokens and as many tiles as compute units the down product reads the weights faster without tiles (figures in ffn_mxfp4_few.hip; beyond: 64
+// experts, 512 rows, 2048 x 1024, 1024 tiles, 20 us against 17.5; 8 experts, 256 rows, 4096 x 14336 57 against 52).  0: tiles; else the
+// experts that can have rows.
+static int few_rows_experts(const dynmo_desc* d) {
+  const int64_t rows = (int64_t)d->T * d->k, experts = rows < d->E ? rows : d->E;
+  return d->T <= 64 && experts * ((d->H + 127) / 128) <= 256 ? (int)experts : 0;
+}
+// Whether the row blocks and both products' tiles fit launches: asked before the first one is made
+static bool mx_fits(const dynmo_desc* d) {
+  return mx_max_row_blocks(d) < kMaxBlocks && !too_many_tiles<true>(d) && (few_rows_experts(d) || !too_many_tiles<false>(d));
 }
 
 struct MxWorkspace {
@@ -264,7 +285,7 @@ extern "C" int32_t dynmo_grouped_ffn_mxfp4(const dynmo_desc* d, const void* x, c
   const int32_t rc = check_desc(d);
   if (rc) return rc;
   if (d->dtype != DYNMO_BF16) return DYNMO_EUNSUPPORTED;
-  if (d->H > 1 << 22 || d->F > 1 << 22) return DYNMO_EUNSUPPORTED;  // a tile's row blocks are addressed with 32-bit byte offsets
+  if (d->H > 1 << 22 || d->F > 1 << 22 || !mx_fits(d)) return DYNMO_EUNSUPPORTED;  // a tile's row blocks are addressed with 32-bit byte offsets
   if (!x || !seg_offsets || !Wg || !Wu || !Wd || !y_p || !workspace || !G_save != !U_save) return DYNMO_EINVAL;
   if (misaligned16(x, Wg, Wu, Wd, y_p, G_save, U_save)) return DYNMO_EINVAL;
   const MxWorkspace w = mx_workspace(d);
@@ -296,11 +317,7 @@ extern "C" int32_t dynmo_grouped_ffn_mxfp4(const dynmo_desc* d, const void* x, c
   p.W1 = (const char*)Wd;
   p.w_bytes = mx_bytes(d->H, d->F);
   p.C0 = (bf16_t*)y_p;
-  // Up to 64 tokens and as many tiles as compute units the weights are read faster without tiles (figures in ffn_mxfp4_few.hip; beyond: 64
-  // experts, 512 rows, 2048 x 1024, 1024 tiles, 20 us against 17.5; 8 experts, 256 rows, 4096 x 14336 57 against 52).
-  const int64_t rows = (int64_t)d->T * d->k;
-  const int max_experts = (int)(rows < d->E ? rows : d->E);
-  if (d->T <= 64 && (int64_t)max_experts * ((d->H + 127) / 128) <= 256) return mx_few_rows(p, max_experts, K_FFN_DOWN, st);
+  if (const int experts = few_rows_experts(d)) return mx_few_rows(p, experts, K_FFN_DOWN, st);
   return mx_tiles<false>(p, d, K_FFN_DOWN, st);
 }
 
@@ -315,7 +332,7 @@ extern "C" int32_t dynmo_grouped_ffn_mxfp4_bwd(const dynmo_desc* d, const void* 
                                                void* workspace, size_t workspace_bytes, void* stream) {
   const int32_t rc = check_desc(d);
   if (rc) return rc;
-  if (d->dtype != DYNMO_BF16 || d->H > 1 << 22 || d->F > 1 << 22 || mx_max_row_blocks(d) >= kMaxBlocks) return DYNMO_EUNSUPPORTED;
+  if (d->dtype != DYNMO_BF16 || d->H > 1 << 22 || d->F > 1 << 22 || !mx_fits(d)) return DYNMO_EUNSUPPORTED;
   if (!fwd_workspace || !workspace) return DYNMO_EINVAL;
   const MxWorkspace w = mx_workspace(d);
   if (fwd_workspace_bytes < w.bytes || workspace_bytes < dynmo_grouped_ffn_mxfp4_bwd_workspace_bytes(d)) return DYNMO_EWORKSPACE;

@@ -103,7 +103,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ffn_mx_few_kernel(const MxP
 }
 
 int32_t mx_few_rows(const MxProduct& p, int max_experts, KernelId id, hipStream_t st) {
-  if (max_experts <= 0) return DYNMO_OK;
   const dim3 grid((p.N + 16 * kFewBlocks - 1) / (16 * kFewBlocks), max_experts);
   DYNMO_TIMED_LAUNCH(id, st, ffn_mx_few_kernel<<<grid, dim3(64 * kFewWaves), 0, st>>>(p));
   return DYNMO_OK;

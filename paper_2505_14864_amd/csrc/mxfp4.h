@@ -41,7 +41,7 @@ int32_t mx_quantize_segments(const dynmo_desc* d, const void* x, const int32_t* 
 int32_t mx_dequantize_segments(const dynmo_desc* d, const void* codes, const void* scales, const int32_t* seg, int K, bf16_t* dst, hipStream_t st);
 
 constexpr int64_t kMaxBlocks = 1 << 24;  // workgroups of 256 threads: a launch has fewer than 2^32
-// The most row blocks that the segments can have
+// The most row blocks that the segments can have; the callers of the two above refuse kMaxBlocks and more
 inline int64_t mx_max_row_blocks(const dynmo_desc* d) {
   const int64_t rows = (int64_t)d->T * d->k;
   return rows / 16 + (rows < d->E ? rows : d->E);

@@ -211,7 +211,6 @@ int32_t mx_quantize_segments(const dynmo_desc* d, const void* x, const int32_t* 
                              hipStream_t st) {
   const int64_t row_blocks = mx_max_row_blocks(d);
   if (row_blocks == 0) return DYNMO_OK;
-  if (row_blocks >= kMaxBlocks) return DYNMO_EUNSUPPORTED;
   const int parts = parts_of(row_blocks, K);
   DYNMO_TIMED_LAUNCH(K_MXFP4_QUANTIZE, st, mx_quantize_segments_kernel<bf16_t><<<dim3((unsigned)(row_blocks * parts)), dim3(kQuantThreads), 0, st>>>(
                                                (const bf16_t*)x, gather, d->k, seg, d->E, K, parts, (char*)codes, (char*)scales));
@@ -221,7 +220,6 @@ int32_t mx_quantize_segments(const dynmo_desc* d, const void* x, const int32_t* 
 int32_t mx_dequantize_segments(const dynmo_desc* d, const void* codes, const void* scales, const int32_t* seg, int K, bf16_t* dst, hipStream_t st) {
   const int64_t row_blocks = mx_max_row_blocks(d);
   if (row_blocks == 0) return DYNMO_OK;
-  if (row_blocks >= kMaxBlocks) return DYNMO_EUNSUPPORTED;
   const int parts = parts_of(row_blocks, K);
   DYNMO_TIMED_LAUNCH(K_MXFP4_DEQUANTIZE, st, mx_dequantize_segments_kernel<bf16_t><<<dim3((unsigned)(row_blocks * parts)), dim3(kQuantThreads), 0, st>>>(
                                                  (const char*)codes, (const char*)scales, seg, d->E, K, parts, dst));

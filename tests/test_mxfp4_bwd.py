@@ -141,6 +141,17 @@ def test_refusals_without_a_gpu():
     assert B.dynmo_grouped_ffn_mxfp4_bwd_workspace_bytes(d) >= B.dynmo_grouped_ffn_bwd_workspace_bytes(d) + 16 * 16 * 2
 
 
+@pytest.mark.parametrize("T,H,F,E", [(1 << 20, 8, 1 << 22, 4),   # gate/up
+                                     (1 << 20, 1 << 22, 8, 4),   # the down product alone
+                                     (1 << 14, 16, 1 << 22, 64), (1 << 14, 1 << 22, 16, 64)])
+def test_too_many_tiles_are_refused_before_anything_is_launched(T, H, F, E):
+    """Without a GPU a launch gives another error than the refusal."""
+    d, room = B.make_desc(T, H, F, E, 1 if T > 1 << 14 else 16, "bf16"), 1 << 60
+    fwd, bwd = B.lib().dynmo_grouped_ffn_mxfp4, B.lib().dynmo_grouped_ffn_mxfp4_bwd
+    assert fwd(B.C.byref(d), 16, None, 16, 16, 16, 16, 16, None, None, 16, room, None) == -2
+    assert bwd(B.C.byref(d), 16, 16, room, *[16] * 10, 16, room, None) == -2
+
+
 # ---- the GPU ----------------------------------------------------------------------------------------------------------------
 
 def at_offset(n, at):
