@@ -134,7 +134,7 @@ int32_t dynmo_route_topk_all_bwd(const dynmo_desc* d, const float* dgate, const 
  * An expert whose logit is NaN or -inf, or whose v is, is never chosen, and its score is zero; a logit of +inf counts as the
  * largest finite number.  A slot for which no expert is left gets expert_idx -1 and gate_w 0 (a group with fewer than
  * group_best experts that can be chosen counts those it has).
- * Needs E a multiple of groups, 1 <= top_groups <= groups and k <= top_groups * (E / groups), T below 2^26; E up to 256 here, for a caller
+ * Needs E a multiple of groups, 1 <= top_groups <= groups and k <= top_groups * (E / groups), T below 2^26 (for E above 64 up to 2^26 - 4); E up to 256 here, for a caller
  * who routes over the experts of several workers and maps the indices to its own (and to -1) before dynmo_permute.
  * logits [T,E] -> expert_idx [T,k], gate_w [T,k].
  *

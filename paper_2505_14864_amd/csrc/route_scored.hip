@@ -520,12 +520,15 @@ __global__ __launch_bounds__(256) void route_scored_bwd_kernel(const float* __re
   }
 }
 
+static int64_t blocks_of(int T, int tokens_per_wave) { return (T + 4L * tokens_per_wave - 1) / (4L * tokens_per_wave); }
+
 static int32_t check_route(const dynmo_desc* d, const dynmo_route_rule* r) {
   const int32_t rc = check_desc(d, kMaxRouteExperts);
   if (rc) return rc;
   if (!r || (r->score != DYNMO_SCORE_SOFTMAX && r->score != DYNMO_SCORE_SIGMOID)) return DYNMO_EINVAL;
   if (r->groups < 1 || d->E % r->groups || r->top_groups < 1 || r->top_groups > r->groups) return DYNMO_EINVAL;
-  if (d->T >= 1 << 26) return DYNMO_EUNSUPPORTED;  // 2^24 workgroups of four tokens: a launch has fewer than 2^32 threads
+  if (d->T >= 1 << 26) return DYNMO_EUNSUPPORTED;
+  if (d->E > 64 && blocks_of(d->T, 1) >= 1 << 24) return DYNMO_EUNSUPPORTED;  // forward, workgroups of four tokens: a launch has fewer than 2^32 threads
   if (r->group_best < 1 || r->group_best > 2 || (r->renormalize != 0 && r->renormalize != 1)) return DYNMO_EINVAL;
   if (!(r->scale - r->scale == 0.f)) return DYNMO_EINVAL;                  // NaN or infinite
   if (d->k > r->top_groups * (d->E / r->groups)) return DYNMO_EINVAL;  // more slots than experts that can be chosen
@@ -547,8 +550,6 @@ static int32_t by_experts(int E, bool aligned, F&& f) {
   else return with(integral_constant<int, 16>{}, integral_constant<int, 16>{});
 }
 
-static unsigned blocks_of(int T, int tokens_per_wave) { return (unsigned)((T + 4L * tokens_per_wave - 1) / (4L * tokens_per_wave)); }
-
 }  // namespace dynmo
 
 using namespace dynmo;
@@ -562,7 +563,7 @@ extern "C" int32_t dynmo_route_scored(const dynmo_desc* d, const dynmo_route_rul
   return by_experts<false>(d->E, !misaligned16(logits), [&](auto lpt, auto, auto vec) -> int32_t {
     constexpr int LPT = decltype(lpt)::value;
     hipStream_t st = (hipStream_t)stream;
-    DYNMO_TIMED_LAUNCH(K_ROUTE_TOPK, st, route_scored_kernel<LPT, decltype(vec)::value><<<dim3(blocks_of(d->T, 64 / LPT)), dim3(256), 0, st>>>(
+    DYNMO_TIMED_LAUNCH(K_ROUTE_TOPK, st, route_scored_kernel<LPT, decltype(vec)::value><<<dim3((unsigned)blocks_of(d->T, 64 / LPT)), dim3(256), 0, st>>>(
                                              logits, bias, expert_idx, gate_w, d->T, d->E, d->k, *rule));
     return DYNMO_OK;
   });
@@ -578,7 +579,7 @@ extern "C" int32_t dynmo_route_scored_bwd(const dynmo_desc* d, const dynmo_route
     constexpr int LPT = decltype(lpt)::value, VPL = decltype(vpl)::value;
     hipStream_t st = (hipStream_t)stream;
     DYNMO_TIMED_LAUNCH(K_ROUTE_TOPK_BWD, st,
-                       route_scored_bwd_kernel<LPT, VPL, decltype(vec)::value><<<dim3(blocks_of(d->T, 64 / LPT)), dim3(256), 0, st>>>(
+                       route_scored_bwd_kernel<LPT, VPL, decltype(vec)::value><<<dim3((unsigned)blocks_of(d->T, 64 / LPT)), dim3(256), 0, st>>>(
                            dgate, logits, expert_idx, dlogits, d->T, d->E, d->k, *rule));
     return DYNMO_OK;
   });

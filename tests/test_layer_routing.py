@@ -57,6 +57,15 @@ def test_the_gradient_is_that_of_the_last_routing(monkeypatch):
     assert gradient_of(logits, rule=other) is other
 
 
+@pytest.mark.parametrize("E", [65, 256])
+@pytest.mark.parametrize("T", [(1 << 26) - 3, (1 << 26) - 1])
+def test_batches_too_long_for_a_launch_are_refused(E, T):
+    """Above 64 experts a workgroup has four tokens, and 2^24 of those are 2^32 threads.  Without a GPU a launch gives another error."""
+    d, rule = B.C.byref(B.make_desc(T, 8, 8, E, 2, "bf16")), B.C.byref(B.make_rule())
+    assert B.lib().dynmo_route_scored(d, rule, 16, None, 16, 16, None) == -2
+    assert B.lib().dynmo_route_scored_bwd(d, rule, 16, 16, 16, 16, None) == -2
+
+
 @pytest.mark.gpu
 def test_gradient_of_a_binding_call_behind_a_scored_routing():
     T, E, k = 40, 6, 2
