@@ -452,7 +452,7 @@ __global__ __launch_bounds__(256) void route_scored_bwd_kernel(const float* __re
 #pragma unroll
   for (int q = 0; q < VPL; q += 4) *(u32x4*)(row + expert_of<LPT>(q, j)) = u32x4{0u, 0u, 0u, 0u};
   wave_lds_order();
-  // slot `n` of the token: its expert (-1: none), that expert's logit and the gradient
+  // slot `n` of the token: its expert (-1: none), that expert's logit and the gradient before its scaling
   auto slot = [&](int n, float* x, float* g) {
     *x = -INFINITY;
     *g = 0.f;
@@ -460,20 +460,29 @@ __global__ __launch_bounds__(256) void route_scored_bwd_kernel(const float* __re
     const int e = expert_idx[t * k + n];
     if (e < 0 || e >= E) return -1;
     *x = clean_logit(lg[e]);
-    *g = dgate[t * k + n] * rule.scale;
+    *g = dgate[t * k + n];
     return e;
   };
   float x, g;
   int e = slot(j, &x, &g);  // with more slots than lanes they are looked up again
+  // What all the gradients of renormalised weights have in common has no effect; that of some slot with an expert is taken off all of them, so
+  // that one chosen expert, or equal gradients, give zero and not the rounding of a difference.
+  float common = 0.f;
   if (rule.renormalize) {
+    float some = g;
     top = x;
     for (int n = j + LPT; n < k; n += LPT) {
       slot(n, &x, &g);
+      some = top > -INFINITY ? some : g;
       top = fmaxf(top, x);
     }
+    const unsigned long long have = __ballot(top > -INFINITY) >> (lane - j) & ((1ull << LPT) - 1ull);
+    some = __shfl(some, have ? lane - j + __builtin_ctzll(have) : lane, 64);
+    common = have ? some : 0.f;
     top = max_over<LPT>(top);
     if (!softmax) top = fminf(top, 0.f);
   }
+  auto scaled = [&](float v) { return (v - common) * rule.scale; };
   auto score = [&](float v) {  // in units of e^top (not all: 1)
     if (v == -INFINITY) return 0.f;
     if (softmax) return __expf(v - top) * inv;
@@ -483,16 +492,16 @@ __global__ __launch_bounds__(256) void route_scored_bwd_kernel(const float* __re
   for (int n = j; n < k; n += LPT) {
     if (k > LPT) slot(n, &x, &g);
     total += score(x);
-    inner += g * score(x);
+    inner += x > -INFINITY ? scaled(g) * score(x) : 0.f;
   }
   total = sum_over<LPT>(total);
   inner = sum_over<LPT>(inner);
   const float by = !rule.renormalize ? 1.f : total > 0.f ? 1.f / total : 0.f;
   for (int base = 0; base < k; base += LPT) {
     if (k > LPT) e = slot(base + j, &x, &g);
-    float d = g;  // all: what the expert's own score is multiplied with below
-    if (!all) d = score(x) * by * (rule.renormalize ? g - inner * by : g) * (softmax ? 1.f : sigmoidf_(-x));
-    if (!all && x == -INFINITY) d = 0.f;
+    float d = scaled(g);  // all: what the expert's own score is multiplied with below
+    if (!all) d = score(x) * by * (rule.renormalize ? d - inner * by : d) * (softmax ? 1.f : sigmoidf_(-x));
+    if (x == -INFINITY) d = 0.f;
     for (int i = 0; i < LPT && base + i < k; ++i) {
       if (j == i && e >= 0) __hip_atomic_fetch_add(row + e, d, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
       wave_lds_order();

@@ -98,3 +98,32 @@ def test_scored_routing_of_a_layer_with_a_residual(mode):
         assert np.array_equal(layer.expert_idx.cpu().numpy(), idx)
         ref = orc.route_scored_bwd(dg, lg, idx, score, renormalize)
         assert np.abs(layer.route_bwd(logits).cpu().numpy() - ref).max() <= 64 * 2.0 ** -24 * 2 * np.abs(dg).sum(1).max()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("E", [8, 40, 100, 256])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("scale", [1.0, 2.3])
+def test_gradients_that_renormalised_weights_do_not_pass_on(E, score, scale):
+    """One chosen expert has the weight `scale` whatever its logit, and what all of a token's gradients have in common changes nothing: zero, not
+    the rounding of a difference.  Where they differ a little the result is as exact as the differences: 64 * 2^-24 of them."""
+    T = 45
+    rng = np.random.default_rng(E)
+    lg = (3 * rng.standard_normal((T, E))).astype(np.float32)
+
+    def grad(idx, dg):
+        out = torch.full((T, E), 7.0, dtype=torch.float32, device="cuda")
+        B.dynmo_route_scored_bwd(B.make_desc(T, 8, 8, E, idx.shape[1], "bf16"), B.make_rule(score, scale=scale), torch.from_numpy(dg).cuda(),
+                                 torch.from_numpy(lg).cuda(), torch.from_numpy(idx).cuda(), out)
+        return out.cpu().numpy()
+
+    for k in (1, 5, min(E, 40)):
+        idx, _ = orc.route_scored(lg, None, k, score)
+        dg = rng.standard_normal((T, k)).astype(np.float32)
+        lone = np.full_like(idx, -1)
+        lone[np.arange(T), rng.integers(0, k, T)] = idx[:, 0]  # the other slots were dropped
+        assert (grad(lone, dg) == 0).all()
+        assert (grad(idx, np.repeat(dg[:, :1], k, 1)) == 0).all()
+        dg = (100 * rng.standard_normal((T, 1)) + dg).astype(np.float32)
+        apart = np.abs(dg.astype(np.float64) - dg[:, :1]).sum(1, keepdims=True)
+        assert (np.abs(grad(idx, dg) - orc.route_scored_bwd(dg, lg, idx, score, True, scale)) <= 64 * 2.0 ** -24 * 2 * scale * apart).all()
