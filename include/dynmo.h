@@ -330,8 +330,8 @@ size_t dynmo_grouped_ffn_mxfp4_bwd_workspace_bytes(const dynmo_desc* d);
  * included): dA = dY Wd; dG = dA U silu'(G); dU = dA silu(G); dX = dG Wg + dU Wu; dWd[e] = dY_e^T Q(A)_e; dWg[e] = dG_e^T Q(X)_e; dWu[e] = dU_e^T Q(X)_e.
  * fwd_workspace: the forward call's, as that call on the same descriptor and segments left it (not a copy at another address): it holds Q(X) and Q(A).
  * G_save, U_save: of that call.  Wg, Wu [E,F,H], Wd [E,H,F] in bfloat16, as dynmo_mxfp4_dequantize gives them.  Everything else as for
- * dynmo_grouped_ffn_bwd, whose weight gradients after that forward call would be those of the X and silu(G) U that were not quantised.  DYNMO_BF16
- * only, limits as for the forward call. */
+ * dynmo_grouped_ffn_bwd, whose weight gradients after that forward call would be those of the X and silu(G) U that were not quantised; workspace is
+ * another one than fwd_workspace, which is left as it is.  DYNMO_BF16 only, limits as for the forward call. */
 int32_t dynmo_grouped_ffn_mxfp4_bwd(const dynmo_desc* d, const void* dy_p, const void* fwd_workspace, size_t fwd_workspace_bytes,
                                     const void* G_save, const void* U_save, const int32_t* seg_offsets, const void* Wg, const void* Wu,
                                     const void* Wd, void* dx_p, void* dWg, void* dWu, void* dWd, void* workspace, size_t workspace_bytes,

@@ -12,11 +12,14 @@
 // scales of four steps come with every fourth.  A load has a descriptor that stays and a scalar offset that moves: with addresses worked
 // out per load the scalar instructions took 15 % (gate/up of 8192 rows 686 -> 600 us).
 //
-// Bound, 8192 rows over 8 experts, 4096 x 14336: gate/up 3.6 PFLOP/s (534 us), down 3.4 (282), of 6.5 to 7 that the instruction alone reaches on random operands from
-// registers.  Both are held by the chip's power: the clock is at 1.9 GHz here with the matrix pipes busy half of the time, and the same launches on
-// operands of zeros took 443 and 233 us when they took 590 and 291.  What is left at that is the loads (447 and 202 us without them, 355 and 234 without the matrix instructions and
-// the reads).  Measured and no faster: tiles of 256 x 256 by eight wavefronts (603, 324) or by four of 128 x 128 (667, 330), 128 x 256 (595, 293), the next
-// step's operands read from LDS during the present one (609, 304), row tiles walked in chunks of 8, 12 or 16.  Two stages instead of three: down of 256
+// Bound, 8192 rows over 8 experts, 4096 x 14336: gate/up 3.6 PFLOP/s (534 us), down 3.4 (282), of 6.5 to 7 that the instruction alone reaches on random
+// operands from registers.  Counted: the matrix pipes are busy 50 % (down 46 %) of 0.92 M (0.50 M) cycles, at 1.9 GHz.  So a step of a 256 x 128 tile
+// takes some 965 (1050) clocks of a compute unit, its share of the epilogue included, where its matrix instructions need 512 and its LDS traffic, 4 x
+// 12 KB read and 24 KB written at 128 bytes a clock, 576: neither is full, LDS is the fuller one, and the rest is where the two do not overlap.  For a
+// 128 x 128 tile it is 256 against 384.  The clock is lowered by the chip's power: on operands of zeros the same launches took 443 and 233 us
+// when they took 590 and 291.  447 and 202 us without the loads, 355 and 234 without the matrix instructions and the reads.
+// Measured and no faster: tiles of 256 x 256 by eight wavefronts (603, 324) or by four of 128 x 128 (667, 330), 128 x 256 (595, 293), the next step's
+// operands read from LDS during the present one (609, 304), row tiles walked in chunks of 8, 12 or 16.  Two stages instead of three: down of 256
 // rows 51 -> 83 us; four: a workgroup less per compute unit, gate/up of 64 ragged experts 67 -> 75, of 2000 rows 165 -> 215.
 // Few rows: bound by reading the weights once (64 rows over 8 experts, gate/up 84 us, 6 TB/s).
 #include "ffn_mxfp4.h"
@@ -243,9 +246,11 @@ template <bool GATEUP>
 static bool too_many_tiles(const dynmo_desc* d) {
   return (takes_wide<GATEUP>(d) ? mx_tile_count<GATEUP, Wide>(d) : mx_tile_count<GATEUP, Narrow>(d)) > kMaxTiles;
 }
-// Up to 64 tokens and as many tiles as compute units the down product reads the weights faster without tiles (figures in ffn_mxfp4_few.hip; beyond: 64
-// experts, 512 rows, 2048 x 1024, 1024 tiles, 20 us against 17.5; 8 experts, 256 rows, 4096 x 14336 57 against 52).  0: tiles; else the
-// experts that can have rows.
+// Up to 64 tokens and as many tiles as compute units the down product reads the weights faster without tiles (figures in ffn_mxfp4_few.hip; more
+// tokens: 8 experts, 256 rows, 4096 x 14336 57 against 52).  From 512 tiles on it depends on the length of the sum and little is at stake; the whole call, us,
+// tiles / without: 16 experts, 4096 x 14336, 16 rows 180 / 177, 128 rows 259 / 258; 16, 4096 x 2048, 16 rows 31.8 / 32.2, 256 rows 39.5 / 40.7; 8, 8192 x 8192, 64 rows
+// 147 / 150; 32, 4096 x 4096, 128 rows, 1024 tiles 153 / 150; 64, 2048 x 1408, 384 rows, 1024 tiles 59.8 / 65.4.
+// 0: tiles; else the experts that can have rows.
 static int few_rows_experts(const dynmo_desc* d) {
   const int64_t rows = (int64_t)d->T * d->k, experts = rows < d->E ? rows : d->E;
   return d->T <= 64 && experts * ((d->H + 127) / 128) <= 256 ? (int)experts : 0;

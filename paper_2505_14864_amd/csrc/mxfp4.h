@@ -37,7 +37,8 @@ __device__ __forceinline__ float mx_scale_value(uint32_t byte) { return __uint_a
 // expert (an expert's last block fewer), the experts' blocks one after another; `gather`: row p is x[gather[p] / gather_div], or nullptr.
 int32_t mx_quantize_segments(const dynmo_desc* d, const void* x, const int32_t* gather, const int32_t* seg, int K, void* codes, void* scales,
                              hipStream_t st);
-// The reverse, for rows that are read next: row p of `dst` [T*k, K] becomes the values that its codes stand for; rows behind the last segment are left as they are.
+// The reverse, for rows that are read next: row p of `dst` [T*k, K] becomes the values that its codes stand for; rows behind the last segment are
+// left as they are.
 int32_t mx_dequantize_segments(const dynmo_desc* d, const void* codes, const void* scales, const int32_t* seg, int K, bf16_t* dst, hipStream_t st);
 
 constexpr int64_t kMaxBlocks = 1 << 24;  // workgroups of 256 threads: a launch has fewer than 2^32

@@ -188,6 +188,7 @@ __global__ __launch_bounds__(kQuantThreads) void mx_quantize_segments_kernel(con
                    scales + (size_t)rb * Kq * kMxScales);
 }
 
+// Bound by memory; 8192 rows of 4096 and 14336 values 28 and 90 us (3 to 3.3 TB/s), beside weight gradients of 850 us each.
 template <typename T>
 __global__ __launch_bounds__(kQuantThreads) void mx_dequantize_segments_kernel(const char* __restrict__ codes, const char* __restrict__ scales,
                                                                                const int32_t* __restrict__ seg, int E, int K, int parts,
